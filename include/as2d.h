@@ -166,6 +166,150 @@ int as2d_verify_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const int32
  */
 int as2d_verify_static(as2d_ctx* ctx, int32_t req, const int32_t* cands, int32_t k, as2d_verify_out* out);
 
+/*
+ * Trees of candidates.  Candidate i follows candidate parents[i] < i, or the
+ * root where parents[i] = -1; parents = NULL is the chain 0, 1, 2, ...  In a
+ * pass over a tree the rows take the cache rows kv_len .. kv_len + k in order,
+ * a row's rotary position is kv_len and its depth, and it attends to the
+ * committed positions, its ancestors and itself.  The accepted path's rows are
+ * then moved together, so that the cache holds what a chain would have left.
+ *
+ * as2d_verify_tree: the walk starts at the root and goes on to the
+ * lowest-numbered child that equals its node's greedy token while there is
+ * one.  out->accepted_len is the path's length, out->correction_token the
+ * greedy token after its last row; path (optional, k entries) receives the
+ * accepted candidates' numbers, then -1.  A chain gives what as2d_verify gives,
+ * bit for bit.  Sibling candidates change the order of a row's attention sums
+ * (hidden keys between the visible ones), so logits along a tree's path equal
+ * a chain's to rounding.
+ *
+ * as2d_verify_sampled: instead of comparing with greedy tokens, each node's
+ * children are tested in order against the target's probabilities with given
+ * random numbers (as2d_sampler_verify has the rule), so that the committed
+ * tokens follow the target's distribution at the temperature.
+ *
+ * as2d_verify_tree_batch: n requests in one pass as in as2d_verify_batch, with
+ * parents_flat and paths_flat laid out as cands_flat (parents_flat = NULL: all
+ * chains; paths_flat may be NULL); sampling = NULL: greedy, else n entries.
+ *
+ * Errors, per-request non-finite logits and limits as in as2d_verify_batch
+ * (AS2D_EINVAL also for a parent that does not come before its child, a
+ * temperature that is not positive and finite, a random number outside [0, 1)).
+ * Passes over trees run as AS2D_EXEC_GRAPH where the mode is
+ * AS2D_EXEC_PERSISTENT.  A sampling call allocates device memory at its first
+ * use and when a call needs more (the drafter's logits it copies, and a
+ * workspace of about 40 bytes per row and 4,096 tokens).
+ */
+typedef struct {
+  double temperature;        /* > 0: p = softmax(logits / temperature) */
+  double draft_temperature;  /* of the drafter's logits; 0: temperature */
+  const float* uniforms;     /* host, k + 1 numbers in [0, 1): [i] tests candidate i, [k] draws the token after the path */
+  const float* draft_logits; /* host or device, or NULL (candidates that come with no distribution): [.][vocab], row r the
+                                logits that the children of row r (0 the root, i + 1 candidate i) were drawn from; rows up
+                                to the last one with children */
+} as2d_sampling;
+
+int as2d_verify_tree(as2d_ctx* ctx, int32_t req, const int32_t* cands, const int32_t* parents, int32_t k,
+                     as2d_verify_out* out, int32_t* path);
+int as2d_verify_sampled(as2d_ctx* ctx, int32_t req, const int32_t* cands, const int32_t* parents, int32_t k,
+                        const as2d_sampling* sampling, as2d_verify_out* out, int32_t* path);
+int as2d_verify_tree_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const int32_t* cands_flat,
+                           const int32_t* parents_flat, const int32_t* ks, const as2d_sampling* sampling,
+                           as2d_verify_out* outs, int32_t* paths_flat);
+
+/*
+ * Operators on one layer of a request's cache, for programs that run layers of
+ * their own beside the library (draft heads that read the target's cache,
+ * caches that arrive from another process).  Tensors are device memory,
+ * [rows][heads][head_dim] with adjacent dimensions and any row and head
+ * strides (in elements).  The call is ordered on hip_stream (NULL: the default
+ * stream) of the context's device and returns before it has run; the
+ * context's other calls wait for it, and these calls for each other, whatever
+ * their streams.  They cannot be captured into a graph (AS2D_ESTATE).
+ *
+ * as2d_tree_attention: attention of n_rows <= 32 rows of a tree (row 0 the
+ * root; parents, host, n_rows - 1 entries or NULL, as above) over positions
+ * 0 .. kv_len - 1 of the request and the rows' ancestors and themselves, with
+ * scores scaled by 1 / sqrt(head_dim).  q, out: [n_rows][n_q_heads][head_dim];
+ * k, v: [n_rows][n_kv_heads][head_dim]; all in cfg->dtype, q and k already
+ * rotated.  k and v are put into the layer's cache rows kv_len .. (kv_len stays
+ * as it is, later calls overwrite them).  kv_len + n_rows <= max_kv_len (else
+ * AS2D_ECAPACITY).  A pass of as2d_verify_tree runs the same kernels.
+ *
+ * as2d_write_kv: keys (rotated) and values of positions pos .. pos + n_tok - 1
+ * <= kv_len - 1 of the layer, [n_tok][n_kv_heads][head_dim] in `dtype`
+ * (AS2D_F32 or AS2D_BF16): the counterpart of as2d_read_kv.
+ */
+typedef struct {
+  void* data;
+  int64_t row_stride, head_stride;
+} as2d_rows;
+
+int as2d_tree_attention(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t n_rows, const int32_t* parents,
+                        const as2d_rows* q, const as2d_rows* k, const as2d_rows* v, const as2d_rows* out,
+                        void* hip_stream);
+int as2d_write_kv(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t pos, int32_t n_tok, int32_t dtype,
+                  const as2d_rows* k, const as2d_rows* v, void* hip_stream);
+
+/*
+ * Sampler: verification of drafted tokens against the target's probabilities
+ * from given random numbers, on device tensors, for programs that have the
+ * logits already.
+ *
+ * Request r has rows r (k + 1) .. of logits: the root's and its candidates'.
+ * p = softmax(logits / temperature) of a row; q = softmax(draft_logits /
+ * draft_temperature) of the row its children were drawn from, each a draw of
+ * its own.  From the root on, at a node with R = p, S = 1, its children in
+ * order: child i with token x is accepted where
+ *   uniforms[i] S q(x) < R(x)
+ * and the walk goes on there; else R <- max(R - S q, 0), S <- sum R.  Without
+ * draft_logits q is 1 at x: R(x) <- 0.  After the last child the token is the
+ * first j with R_0 + .. + R_j > uniforms[k] S; where nothing is left of R, R = p
+ * again.  Each committed token then follows p.
+ *
+ * A logit of -inf is a token of probability 0.  A request with a NaN or +inf
+ * in a row (rows without children of draft_logits and rows past ks[r] are not
+ * read), a row of -inf alone, ks[r] outside [0, k] or a temperature that is not
+ * positive and finite gets accepted = token = -1, its path -1 and its logp NaN.
+ * A candidate outside [0, vocab) is never accepted.
+ *
+ * as2d_sampler_create allocates the workspace of calls of up to max_requests
+ * <= 4096 requests, max_k <= 31 candidates and max_vocab <= 2^24 tokens on the
+ * current device.  as2d_sampler_verify is ordered on hip_stream and returns
+ * before it has run; it may be captured into a graph.  Calls of one sampler
+ * share the workspace: calls on several streams are ordered by the library,
+ * captured calls by whoever replays the graphs.  One host thread at a time.
+ * Errors: AS2D_EINVAL, AS2D_EHIP, AS2D_ENOMEM; as2d_sampler_last_error(NULL) has
+ * the message of a failed create.
+ */
+typedef struct as2d_sampler as2d_sampler;
+
+typedef struct {
+  int32_t n, k, vocab;          /* requests (0: nothing is done), candidates each, tokens */
+  int32_t dtype;                /* of both logits: AS2D_F32 or AS2D_BF16 */
+  const void* logits;           /* [n][k + 1] rows, row_stride elements apart */
+  int64_t row_stride;           /* >= vocab */
+  const void* draft_logits;     /* the same of the drafter, or NULL */
+  int64_t draft_row_stride;
+  const int32_t* cands;         /* [n][k] */
+  const int32_t* parents;       /* HOST, [k], of every request's tree; NULL: chains */
+  const int32_t* ks;            /* [n]: candidates of each request (its first ks[r] of k), or NULL: k */
+  const float* uniforms;        /* [n][k + 1] in [0, 1): [k] draws the token after the path */
+  const float* temperatures;    /* [n], or NULL: `temperature` */
+  double temperature;
+  double draft_temperature;     /* 0: the request's temperature */
+  int32_t* accepted;            /* [n]: candidates on the accepted path */
+  int32_t* path;                /* [n][k]: their numbers, then -1 */
+  int32_t* token;               /* [n]: the token after the path */
+  float* logp;                  /* [n][k + 1] or NULL: log p of each candidate at its parent, [k] of the token
+                                   (NaN past ks[r]) */
+} as2d_sample_args;
+
+int as2d_sampler_create(int32_t max_requests, int32_t max_k, int32_t max_vocab, as2d_sampler** out);
+int as2d_sampler_free(as2d_sampler* sampler);
+int as2d_sampler_verify(as2d_sampler* sampler, const as2d_sample_args* args, void* hip_stream);
+const char* as2d_sampler_last_error(const as2d_sampler* sampler);
+
 /* ---- test and inspection hooks (not on the timed path) ---------------- */
 
 /* When on, later calls also write the float32 logits of every processed

@@ -28,7 +28,10 @@ EXPORTS = ["as2d_load_weights", "as2d_prefill_kv", "as2d_verify", "as2d_decode_o
            "as2d_cbuf_create", "as2d_cbuf_free", "as2d_cbuf_publish", "as2d_cbuf_snapshot",
            "as2d_cbuf_read", "as2d_cbuf_n_records", "as2d_cbuf_get_record", "as2d_cursor_init",
            "as2d_cursor_propose", "as2d_cursor_update", "as2d_verify_from_buffer", "as2d_run_decoupled",
-           "as2d_set_stream", "as2d_set_cu_budget", "as2d_verify_static"]
+           "as2d_set_stream", "as2d_set_cu_budget", "as2d_verify_static",
+           "as2d_verify_tree", "as2d_verify_sampled", "as2d_verify_tree_batch", "as2d_tree_attention",
+           "as2d_write_kv", "as2d_sampler_create", "as2d_sampler_free", "as2d_sampler_verify",
+           "as2d_sampler_last_error"]
 
 
 class Config(ctypes.Structure):
@@ -64,6 +67,24 @@ class ReadCursorC(ctypes.Structure):
 class Interval(ctypes.Structure):
     _fields_ = [("start_ns", ctypes.c_int64), ("end_ns", ctypes.c_int64), ("kind", ctypes.c_int32),
                 ("tokens", ctypes.c_int32)]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_double), ("draft_temperature", ctypes.c_double),
+                ("uniforms", ctypes.c_void_p), ("draft_logits", ctypes.c_void_p)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class SampleArgs(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("k", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("draft_logits", ctypes.c_void_p),
+                ("draft_row_stride", ctypes.c_int64), ("cands", ctypes.c_void_p), ("parents", ctypes.c_void_p),
+                ("ks", ctypes.c_void_p), ("uniforms", ctypes.c_void_p), ("temperatures", ctypes.c_void_p),
+                ("temperature", ctypes.c_double), ("draft_temperature", ctypes.c_double), ("accepted", ctypes.c_void_p),
+                ("path", ctypes.c_void_p), ("token", ctypes.c_void_p), ("logp", ctypes.c_void_p)]
 
 
 class As2dError(RuntimeError):
@@ -127,6 +148,17 @@ def load_library(path: str = LIB_PATH):
                                             ctypes.POINTER(VerifyOut), ctypes.POINTER(_I)]
     lib.as2d_run_decoupled.argtypes = [_P, _I, _P, _I, _P, _I, _I, _I, _I, _P, ctypes.POINTER(ReadCursorC), _P,
                                        _P, _I, ctypes.POINTER(_I), ctypes.POINTER(_L), ctypes.POINTER(_I)]
+    lib.as2d_verify_tree.argtypes = [_P, _I, _P, _P, _I, ctypes.POINTER(VerifyOut), _P]
+    lib.as2d_verify_sampled.argtypes = [_P, _I, _P, _P, _I, ctypes.POINTER(Sampling), ctypes.POINTER(VerifyOut), _P]
+    lib.as2d_verify_tree_batch.argtypes = [_P, _I, _P, _P, _P, _P, ctypes.POINTER(Sampling), _P, _P]
+    _R = ctypes.POINTER(Rows)
+    lib.as2d_tree_attention.argtypes = [_P, _I, _I, _I, _P, _R, _R, _R, _R, _P]
+    lib.as2d_write_kv.argtypes = [_P, _I, _I, _I, _I, _I, _R, _R, _P]
+    lib.as2d_sampler_create.argtypes = [_I, _I, _I, ctypes.POINTER(_P)]
+    lib.as2d_sampler_free.argtypes = [_P]
+    lib.as2d_sampler_verify.argtypes = [_P, ctypes.POINTER(SampleArgs), _P]
+    lib.as2d_sampler_last_error.argtypes = [_P]
+    lib.as2d_sampler_last_error.restype = ctypes.c_char_p
     lib.as2d_set_stream.argtypes = [_P, _P]
     lib.as2d_set_cu_budget.argtypes = [_P, _I]
     lib.as2d_free.argtypes = [_P]
@@ -134,7 +166,7 @@ def load_library(path: str = LIB_PATH):
     lib.as2d_last_error.argtypes = [_P]
     lib.as2d_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
-        if name not in ("as2d_free", "as2d_last_error", "as2d_step_bytes"):
+        if name not in ("as2d_free", "as2d_last_error", "as2d_step_bytes", "as2d_sampler_last_error"):
             getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -142,6 +174,69 @@ def load_library(path: str = LIB_PATH):
 
 def _ptr(a: np.ndarray) -> int:
     return a.ctypes.data
+
+
+_TYPES = {"torch.float32": F32, "torch.bfloat16": BF16}
+
+
+def _refuse(what: str):
+    raise As2dError(EINVAL, what)
+
+
+def _on_device(t, name: str, dtype, shape) -> int:
+    """Checks a device tensor (torch) and returns its address; a None in
+    `shape` stands for any size."""
+    if not getattr(t, "is_cuda", False):
+        _refuse(f"{name}: a device tensor is wanted")
+    if dtype is not None and str(t.dtype) != dtype:
+        _refuse(f"{name}: {dtype} is wanted, not {t.dtype}")
+    if len(t.shape) != len(shape) or any(w is not None and w != s for w, s in zip(shape, t.shape)):
+        _refuse(f"{name}: shape {tuple(shape)} is wanted, not {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _dense(t, name: str, dtype, shape) -> int:
+    p = _on_device(t, name, dtype, shape)
+    if not t.is_contiguous():
+        _refuse(f"{name}: a contiguous tensor is wanted")
+    return p
+
+
+def _rows(t, name: str, dtype, shape) -> Rows:
+    p = _on_device(t, name, dtype, shape)
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        _refuse(f"{name}: adjacent dimensions are wanted")
+    return Rows(p, t.stride(0), t.stride(1))
+
+
+def _same_device(tensors):
+    if len({t.device for t in tensors}) > 1:
+        _refuse("tensors on several devices")
+
+
+def _stream_of(t, stream: Optional[int]) -> int:
+    """The given stream's handle, or the current torch stream of the tensor's device."""
+    if stream is not None:
+        return stream
+    import torch
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _int32(values) -> np.ndarray:
+    return np.ascontiguousarray(values, dtype=np.int32)
+
+
+def _parents(parents, k: int) -> Optional[np.ndarray]:
+    if parents is None:
+        return None
+    p = _int32(parents)
+    if p.shape != (k,):
+        _refuse(f"parents: {k} entries are wanted, not {p.shape}")
+    return p
+
+
+def _opt(a: Optional[np.ndarray]):
+    return _ptr(a) if a is not None and a.size else None
 
 
 class Model:
@@ -225,6 +320,108 @@ class Model:
         outs = (VerifyOut * n)()
         self._check(self.lib.as2d_verify_batch(self.ctx, n, _ptr(r), _ptr(flat), _ptr(ks), outs))
         return [o.as_dict() for o in outs]
+
+    def verify_tree(self, req: int, cands: Sequence[int], parents: Optional[Sequence[int]] = None) -> dict:
+        """One pass over a tree of candidates (parents[i]: the candidate that
+        candidate i follows, -1 the root; None: a chain), greedily verified.
+        The result has the accepted candidates' numbers under "path"."""
+        return self._tree([req], [cands], None if parents is None else [parents], None)[0]
+
+    def verify_sampled(self, req: int, cands: Sequence[int], uniforms, parents: Optional[Sequence[int]] = None,
+                       temperature: float = 1.0, draft_logits=None, draft_temperature: float = 0.0) -> dict:
+        """verify_tree with the candidates tested by sampling: `uniforms` has
+        one number in [0, 1) per candidate and one for the token after the
+        path; draft_logits (numpy or device float32, [rows, vocab]) the logits
+        that the children of each row were drawn from."""
+        return self._tree([req], [cands], None if parents is None else [parents],
+                          [dict(uniforms=uniforms, temperature=temperature, draft_logits=draft_logits,
+                                draft_temperature=draft_temperature)])[0]
+
+    def verify_tree_batch(self, reqs: Sequence[int], cands: Sequence[Sequence[int]],
+                          parents: Optional[Sequence[Optional[Sequence[int]]]] = None,
+                          sampling: Optional[Sequence[dict]] = None) -> List[dict]:
+        """Trees of several requests in one pass; `sampling`: None (greedy) or
+        for each request the keyword arguments of verify_sampled."""
+        return self._tree(reqs, cands, parents, sampling)
+
+    def _tree(self, reqs, cands, parents, sampling):
+        n = len(reqs)
+        cands = [_int32(c) for c in cands]
+        if len(cands) != n or (parents is not None and len(parents) != n) or (sampling is not None and len(sampling) != n):
+            _refuse(f"{n} requests, but not as many candidates, parents or samplings")
+        r, ks = _int32(reqs), _int32([len(c) for c in cands])
+        flat = _int32(np.concatenate(cands)) if n else _int32([])
+        up = None
+        if parents is not None:
+            up = _int32(np.concatenate([_int32(range(-1, len(c) - 1)) if p is None else _parents(p, len(c))
+                                        for p, c in zip(parents, cands)])) if n else None
+        paths = np.full(max(flat.size, 1), -1, np.int32)
+        outs, args, keep = (VerifyOut * max(n, 1))(), None, []
+        if sampling is not None:
+            args = (Sampling * max(n, 1))(*[self._sampling(s, c, p, keep) for s, c, p in
+                                            zip(sampling, cands, parents if parents is not None else [None] * n)])
+        self._check(self.lib.as2d_verify_tree_batch(self.ctx, n, _opt(r), _opt(flat), _opt(up), _opt(ks), args, outs,
+                                                    _ptr(paths)))
+        got, off = [], 0
+        for o, c in zip(outs, cands):
+            got.append(dict(o.as_dict(), path=[int(i) for i in paths[off:off + o.accepted_len]]))
+            off += len(c)
+        return got
+
+    def _sampling(self, s: dict, cands, parents, keep: list) -> Sampling:
+        u = np.ascontiguousarray(s["uniforms"], dtype=np.float32)
+        if u.shape != (len(cands) + 1,):
+            _refuse(f"uniforms: {len(cands) + 1} numbers are wanted, not {u.shape}")
+        keep.append(u)
+        d = s.get("draft_logits")
+        p = None
+        if d is not None and len(cands):
+            rows = max((int(i) + 2 for i in parents), default=1) if parents is not None else len(cands)
+            if len(d.shape) != 2 or d.shape[0] < rows or d.shape[1] != self.shape.vocab:
+                _refuse(f"draft_logits: [{rows} or more, {self.shape.vocab}] is wanted, not {tuple(d.shape)}")
+            if isinstance(d, np.ndarray):
+                d = np.ascontiguousarray(d, dtype=np.float32)
+                p = _ptr(d)
+            else:
+                p = _dense(d, "draft_logits", "torch.float32", (None, self.shape.vocab))
+                import torch
+                torch.cuda.current_stream(d.device).synchronize()   # the pass copies from it on its own stream
+            keep.append(d)
+        return Sampling(s.get("temperature", 1.0), s.get("draft_temperature", 0.0), _ptr(u), p)
+
+    def _model_type(self) -> str:
+        return "torch.float32" if self.shape.dtype == F32 else "torch.bfloat16"
+
+    def tree_attention(self, req: int, layer: int, q, k, v, parents: Optional[Sequence[int]] = None, out=None,
+                       stream: Optional[int] = None):
+        """Attention of a tree's rows over one layer of the request's cache
+        (as2d_tree_attention): q [rows, n_q_heads, head_dim], k and v
+        [rows, n_kv_heads, head_dim], device tensors of the model's type, on
+        the current torch stream or `stream`.  Returns out (new if None)."""
+        s, t, rows = self.shape, self._model_type(), q.shape[0]
+        a = [_rows(q, "q", t, (None, s.n_q_heads, s.head_dim)), _rows(k, "k", t, (rows, s.n_kv_heads, s.head_dim)),
+             _rows(v, "v", t, (rows, s.n_kv_heads, s.head_dim))]
+        if rows < 1:
+            _refuse("tree_attention: no rows")
+        p = _parents(parents, rows - 1)
+        if out is None:
+            out = q.new_empty((rows, s.n_q_heads, s.head_dim))
+        a.append(_rows(out, "out", t, (rows, s.n_q_heads, s.head_dim)))
+        _same_device([q, k, v, out])
+        self._check(self.lib.as2d_tree_attention(self.ctx, req, layer, rows, _opt(p), *a, _stream_of(q, stream)))
+        return out
+
+    def write_kv(self, req: int, layer: int, k, v, pos: int = 0, stream: Optional[int] = None):
+        """Keys and values [n, n_kv_heads, head_dim] (device, float32 or
+        bfloat16) into positions pos .. of one layer of the request's cache."""
+        s = self.shape
+        if str(k.dtype) not in _TYPES:
+            _refuse(f"k: float32 or bfloat16 is wanted, not {k.dtype}")
+        a = [_rows(t, name, str(k.dtype), (k.shape[0], s.n_kv_heads, s.head_dim)) for t, name in ((k, "k"), (v, "v"))]
+        _same_device([k, v])
+        if k.shape[0]:
+            self._check(self.lib.as2d_write_kv(self.ctx, req, layer, pos, k.shape[0], _TYPES[str(k.dtype)], *a,
+                                               _stream_of(k, stream)))
 
     def verify_batch_status(self, reqs: Sequence[int], cands: Sequence[Sequence[int]]):
         """as2d_verify_batch returning (status, per-request results) without
@@ -346,6 +543,86 @@ class Model:
 def _rc(rc, what):
     if rc != OK:
         raise As2dError(rc, what)
+
+
+class Sampler:
+    """Verification of drafted tokens by sampling, on device tensors
+    (as2d_sampler_verify has the rule and the conventions)."""
+
+    def __init__(self, max_requests: int, max_k: int, max_vocab: int):
+        self.lib = load_library()
+        self.h = _P()
+        rc = self.lib.as2d_sampler_create(max_requests, max_k, max_vocab, ctypes.byref(self.h))
+        if rc != OK:
+            raise As2dError(rc, self.lib.as2d_sampler_last_error(None).decode())
+
+    def close(self):
+        if getattr(self, "h", None):
+            self.lib.as2d_sampler_free(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def verify(self, logits, cands, uniforms, parents: Optional[Sequence[int]] = None, ks=None, draft_logits=None,
+               temperature=1.0, draft_temperature: float = 0.0, stream: Optional[int] = None) -> dict:
+        """logits [n, k + 1, vocab] (float32 or bfloat16; rows may be further
+        apart than vocab), draft_logits the same or None, cands [n, k] and ks
+        [n] int32, uniforms [n, k + 1] float32, temperature a number or a
+        float32 tensor [n]: device tensors.  parents: a host list of k entries
+        or None (chains).  Returns device tensors accepted [n], path [n, k],
+        token [n] and logp [n, k + 1], on the current torch stream or
+        `stream`."""
+        import torch
+        if len(getattr(logits, "shape", ())) != 3:
+            _refuse("logits: [n, k + 1, vocab] is wanted")
+        n, rows, vocab = logits.shape
+        k = rows - 1
+        if str(logits.dtype) not in _TYPES or k < 0:
+            _refuse("logits: float32 or bfloat16 and at least one row a request are wanted")
+        a = SampleArgs()
+        a.n, a.k, a.vocab, a.dtype = n, k, vocab, _TYPES[str(logits.dtype)]
+        p = _parents(parents, k)
+        a.parents = _opt(p)
+        tensors = [logits, uniforms]
+        a.logits, a.row_stride = self._logits(logits, "logits", logits)
+        a.uniforms = _dense(uniforms, "uniforms", "torch.float32", (n, rows))
+        if k:
+            a.cands = _dense(cands, "cands", "torch.int32", (n, k))
+            tensors.append(cands)
+        if draft_logits is not None:
+            a.draft_logits, a.draft_row_stride = self._logits(draft_logits, "draft_logits", logits)
+            tensors.append(draft_logits)
+        if ks is not None:
+            a.ks = _dense(ks, "ks", "torch.int32", (n,))
+            tensors.append(ks)
+        if hasattr(temperature, "data_ptr"):
+            a.temperatures = _dense(temperature, "temperature", "torch.float32", (n,))
+            tensors.append(temperature)
+        else:
+            a.temperature = temperature
+        a.draft_temperature = draft_temperature
+        _same_device(tensors)
+        i32 = uniforms.new_empty((n * (k + 2),), dtype=torch.int32)
+        out = dict(accepted=i32[:n], token=i32[n:2 * n], path=i32[2 * n:].view(n, k), logp=uniforms.new_empty((n, rows)))
+        a.accepted, a.token, a.path, a.logp = (out[x].data_ptr() for x in ("accepted", "token", "path", "logp"))
+        rc = self.lib.as2d_sampler_verify(self.h, ctypes.byref(a), _stream_of(logits, stream))
+        if rc != OK:
+            raise As2dError(rc, self.lib.as2d_sampler_last_error(self.h).decode())
+        return out
+
+    @staticmethod
+    def _logits(t, name, like):
+        """(address, elements between rows) of [n, rows, vocab] logits whose rows are evenly apart."""
+        p = _on_device(t, name, str(like.dtype), tuple(like.shape))
+        n, rows, vocab = t.shape
+        step = t.stride(1) if rows > 1 else t.stride(0) if n > 1 else vocab
+        if (vocab > 1 and t.stride(2) != 1) or (n > 1 and rows > 1 and t.stride(0) != rows * step):
+            _refuse(f"{name}: rows of adjacent logits, evenly apart, are wanted")
+        return p, step
 
 
 class CandidateBuffer:

@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <functional>
 #include <map>
 #include <string>
 #include <tuple>
@@ -129,6 +130,24 @@ struct as2d_ctx {
   int h_err = 0;
   long long* ptrace = nullptr;  // persistent-kernel timeline (as2d_set_step_trace)
   int trace_on = 0;
+
+  // passes over trees: the outcome on the device and in pinned memory, what a
+  // sampling pass reads (grown at first use)
+  TreeOut tree{};
+  SampleReq *h_sreq = nullptr, *d_sreq = nullptr;
+  void* sample_work = nullptr;
+  size_t sample_cap = 0;
+  float* draft = nullptr;
+  size_t draft_cap = 0;
+
+  // operators on one cache layer (as2d_tree_attention, as2d_write_kv), which
+  // return before they have run: the stream of the last one
+  int dev = 0;
+  RowDesc* op_rows = nullptr;
+  ReqDesc* op_req = nullptr;
+  hipEvent_t op_ev = nullptr;
+  hipStream_t op_stream = nullptr;
+  bool op_pending = false;
 
   int timing = 0;
   double t_ms[K_COUNT] = {};
@@ -320,6 +339,49 @@ void timing_collect(as2d_ctx* c) {
   c->ev_used.clear();
 }
 
+// The calling thread's device, put back at the end of the scope.
+struct OnDevice {
+  int before = -1;
+  explicit OnDevice(int dev) {
+    int now = 0;
+    if (hipGetDevice(&now) == hipSuccess && now != dev && hipSetDevice(dev) == hipSuccess) before = now;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+// Waits for an operator that another call left running: every other call reads
+// or writes what it does.
+void join_op(as2d_ctx* c) {
+  if (!c->op_pending) return;
+  c->op_pending = false;
+  if (hipStreamSynchronize(c->op_stream) != hipSuccess) {   // the caller may have destroyed its stream
+    (void)hipGetLastError();
+    (void)hipDeviceSynchronize();
+  }
+}
+
+// Before an operator's launches on stream s: after those of an earlier one on
+// another stream (the operators share the context's buffers).
+int begin_op(as2d_ctx* c, hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) != hipSuccess || st != hipStreamCaptureStatusNone) {
+    (void)hipGetLastError();
+    return fail(c, AS2D_ESTATE, "operators on a cache cannot be captured (a replay would keep the cache length)");
+  }
+  hipDevice_t d = c->dev;
+  if (s) HIP_TRY(c, hipStreamGetDevice(s, &d));
+  if (d != c->dev) return fail(c, AS2D_EINVAL, "the stream belongs to device %d, the context to %d", d, c->dev);
+  if (c->op_pending && c->op_stream != s) {
+    if (hipEventRecord(c->op_ev, c->op_stream) == hipSuccess) HIP_TRY(c, hipStreamWaitEvent(s, c->op_ev, 0));
+    else join_op(c);
+  }
+  c->op_pending = true;
+  c->op_stream = s;
+  return AS2D_OK;
+}
+
 int check_req(as2d_ctx* c, int req) {
   if (!c) return AS2D_EINVAL;
   if (req < 0 || req >= c->cfg.max_requests) return fail(c, AS2D_EINVAL, "request id %d out of range", req);
@@ -394,7 +456,7 @@ bool wave_tiles(const as2d_ctx* c, int M, const ReqDesc* reqs, int n, int part_s
 // attention key blocks of any request (it sizes the attention grid); tiles:
 // wave_tiles of the pass.
 int launch_pass(as2d_ctx* c, const PassBufs& B, int M, int n_att, int n_fin, int fin_rows, bool with_head,
-                int max_blocks, bool prefill, bool tiles) {
+                int max_blocks, bool prefill, bool tiles, bool tree = false) {
   const as2d_config& g = c->cfg;
   hipStream_t s = c->stream;
   const bool bf = c->bf16;
@@ -452,6 +514,7 @@ int launch_pass(as2d_ctx* c, const PassBufs& B, int M, int n_att, int n_fin, int
       a.out_plane = B.attn_plane;
       a.M = M;
       a.wave_tiles = tiles;
+      a.tree = tree;
       a.attn_rt = c->attn_rt;
       a.cus = c->grid_cus;
       Timed t(c, K_ATTN);
@@ -512,6 +575,7 @@ int launch_pass(as2d_ctx* c, const PassBufs& B, int M, int n_att, int n_fin, int
       HIP_TRY(c, launch_finish(B.d_rows, B.d_reqs + mr, n_fin, fin_rows, B.amax_val, B.amax_val2, B.amax_idx,
                                g.vocab / kPairCols, B.row_tok, B.row_bad, B.fin_counters,
                                HostOut{c->h_tok, c->h_margin, c->h_out}, s));
+      if (tree) HIP_TRY(c, launch_tree_walk(B.d_rows, B.d_reqs + mr, n_fin, B.row_tok, B.row_bad, c->tree, s));
     }
   }
   return AS2D_OK;
@@ -683,9 +747,10 @@ int launch_persistent(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows) {
 // arguments hold only pointers and sizes (the row and request descriptors
 // are read from device memory when the graph runs) and the attention grid
 // covers the slot capacity, so one graph (two with `tiles`, wave_tiles of the
-// pass) serves every pass of that shape.
-int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persistent, bool tiles, hipGraphExec_t* out) {
-  const auto key = std::make_tuple((int)persistent, M, n_att, 2 * (int)tiles + c->keep_logits);
+// pass, and two for passes over trees) serves every pass of that shape.
+int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persistent, bool tiles, bool tree,
+              hipGraphExec_t* out) {
+  const auto key = std::make_tuple((int)persistent, M, n_att, 4 * (int)tree + 2 * (int)tiles + c->keep_logits);
   auto it = c->graphs.find(key);
   if (it == c->graphs.end()) {
     if (c->graphs.size() >= 128) {
@@ -695,7 +760,7 @@ int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persi
     hipGraph_t gr = nullptr;
     HIP_TRY(c, hipStreamBeginCapture(c->stream, hipStreamCaptureModeThreadLocal));
     int rc = persistent ? launch_persistent(c, M, n_att, n_fin, fin_rows)
-                        : launch_pass(c, c->b, M, n_att, n_fin, fin_rows, true, c->n_blocks_cap, false, tiles);
+                        : launch_pass(c, c->b, M, n_att, n_fin, fin_rows, true, c->n_blocks_cap, false, tiles, tree);
     hipError_t e = hipStreamEndCapture(c->stream, &gr);
     if (rc) {
       if (gr) hipGraphDestroy(gr);
@@ -714,7 +779,11 @@ int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persi
 
 // One forward pass over the rows and requests in h_rows / h_reqs (see
 // launch_pass).  Verification passes run as a captured HIP graph (graph_for).
-int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool verify_call = false) {
+// tree: the rows of trees of candidates (never the persistent kernel); `after`
+// launches what follows the pass before it is waited for.
+int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool verify_call = false, bool tree = false,
+                const std::function<int()>& after = nullptr) {
+  join_op(c);
   const as2d_config& g = c->cfg;
   hipStream_t s = c->stream;
   const int mr = g.max_requests;
@@ -727,7 +796,7 @@ int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool v
   }
   if (max_blocks > c->n_blocks_cap) return fail(c, AS2D_ECAPACITY, "attention blocks %d > %d", max_blocks, c->n_blocks_cap);
   const bool verify_pass = verify_call && with_head && n_fin == n_att;
-  const bool persistent = verify_pass && c->exec_mode == AS2D_EXEC_PERSISTENT && c->pers_ok && c->pers_fit && M <= kStepRows;
+  const bool persistent = verify_pass && !tree && c->exec_mode == AS2D_EXEC_PERSISTENT && c->pers_ok && c->pers_fit && M <= kStepRows;
   const bool graph = verify_pass && c->exec_mode != AS2D_EXEC_EAGER && !c->timing;
   if (persistent && !step_layers_for(c, M)) return fail(c, AS2D_ENOMEM, "persistent step arguments");
   if (persistent || !verify_call) {   // the other passes read and write the host's arrays themselves
@@ -737,12 +806,16 @@ int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool v
   const bool tiles = verify_call && !persistent && wave_tiles(c, M, c->h_reqs, n_att, c->b.part_spans);
   if (graph) {
     hipGraphExec_t ex = nullptr;
-    int rc = graph_for(c, M, n_att, n_fin, fin_rows, persistent, tiles, &ex);
+    int rc = graph_for(c, M, n_att, n_fin, fin_rows, persistent, tiles, tree, &ex);
     if (rc) return rc;
     HIP_TRY(c, hipGraphLaunch(ex, s));
   } else {
     int rc = persistent ? launch_persistent(c, M, n_att, n_fin, fin_rows)
-                        : launch_pass(c, c->b, M, n_att, n_fin, fin_rows, with_head, max_blocks, !verify_call, tiles);
+                        : launch_pass(c, c->b, M, n_att, n_fin, fin_rows, with_head, max_blocks, !verify_call, tiles, tree);
+    if (rc) return rc;
+  }
+  if (after) {
+    const int rc = after();
     if (rc) return rc;
   }
   if (persistent) HIP_TRY(c, hipMemcpyAsync(&c->h_err, c->perr, sizeof(int), hipMemcpyDeviceToHost, s));
@@ -774,7 +847,8 @@ int as2d_prepare_graphs(as2d_ctx* c, int32_t max_rows) {
     for (const int kv_len : {M, std::max(M, c->cfg.max_kv_len)}) {
       const ReqDesc q{0, M, kv_len - M, 0};
       hipGraphExec_t ex = nullptr;
-      const int rc = graph_for(c, M, 1, 1, M, persistent, !persistent && wave_tiles(c, M, &q, 1, c->b.part_spans), &ex);
+      const int rc = graph_for(c, M, 1, 1, M, persistent, !persistent && wave_tiles(c, M, &q, 1, c->b.part_spans), false,
+                               &ex);
       if (rc) return rc;
     }
   }
@@ -871,7 +945,7 @@ int assemble_verify(as2d_ctx* c, int n, const int32_t* reqs, const int32_t* cand
       RowDesc rd{};
       rd.token = i == 0 ? st.root : cands[off + i - 1];
       rd.src = 0;
-      rd.pos = st.kv_len + i;
+      rd.pos = rd.rot = st.kv_len + i;
       rd.slot = reqs[r];
       rd.cmp = i < k ? cands[off + i] : -1;
       c->h_rows[row + i] = rd;
@@ -921,6 +995,147 @@ int commit_verify(as2d_ctx* c, int n, const int32_t* reqs, const int32_t* ks, as
   }
   if (n_bad) return fail(c, AS2D_ENUMERIC, "verify: non-finite logits in %d request(s) (first: %d)", n_bad, first_bad);
   return AS2D_OK;
+}
+
+// Masks of the rows of a tree of k candidates (row 0 the root): parents[i] is
+// the candidate that candidate i follows, -1 the root; null: a chain.  depth
+// (optional): rows' distances from the root; children (optional): the most
+// children of a row.
+int tree_masks(as2d_ctx* c, const char* what, const int32_t* parents, int k, uint32_t* mask, int* depth, int* children) {
+  int n[kStepRows] = {}, d[kStepRows] = {};
+  mask[0] = 1;
+  for (int i = 1; i <= k; ++i) {
+    const int p = parents ? parents[i - 1] : i - 2;
+    if (p < -1 || p >= i - 1)
+      return fail(c, AS2D_EINVAL, "%s: candidate %d follows %d (a parent comes before its children, -1 is the root)", what, i - 1, p);
+    mask[i] = mask[p + 1] | 1u << i;
+    d[i] = d[p + 1] + 1;
+    ++n[p + 1];
+  }
+  if (depth) std::copy(d, d + k + 1, depth);
+  if (children) *children = *std::max_element(n, n + kStepRows);
+  return AS2D_OK;
+}
+
+// The trees of a verification call, after assemble_verify: rotary positions,
+// masks and random numbers of its rows.  *max_k, *max_children: over the
+// requests; *draft: whether one has a drafter's logits.
+int assemble_tree(as2d_ctx* c, int n, const int32_t* parents, const int32_t* ks, const as2d_sampling* sampling, int* max_k,
+                  int* max_children, bool* draft) {
+  int off = 0;
+  for (int r = 0; r < n; off += ks[r++]) {
+    const int k = ks[r];
+    RowDesc* rows = c->h_rows + c->h_reqs[r].row_start;
+    uint32_t mask[kStepRows];
+    int depth[kStepRows], children = 0;
+    const int rc = tree_masks(c, "verify", parents ? parents + off : nullptr, k, mask, depth, &children);
+    if (rc) return rc;
+    for (int i = 0; i <= k; ++i) {
+      rows[i].rot = c->h_reqs[r].L0 + depth[i];
+      rows[i].mask = mask[i];
+    }
+    *max_k = std::max(*max_k, k);
+    *max_children = std::max(*max_children, children);
+    if (!sampling) continue;
+    const as2d_sampling& s = sampling[r];
+    if (!(s.temperature > 0.0) || !std::isfinite(s.temperature) || s.draft_temperature < 0.0 || !std::isfinite(s.draft_temperature))
+      return fail(c, AS2D_EINVAL, "verify: temperature %g, %g of request %d (> 0, and >= 0)", s.temperature, s.draft_temperature, r);
+    if (!s.uniforms) return fail(c, AS2D_EINVAL, "verify: null random numbers");
+    for (int i = 0; i <= k; ++i) {
+      if (!(s.uniforms[i] >= 0.f && s.uniforms[i] < 1.f))
+        return fail(c, AS2D_EINVAL, "verify: random number %g outside [0, 1)", s.uniforms[i]);
+      rows[i < k ? i + 1 : 0].u = s.uniforms[i];
+    }
+    *draft |= s.draft_logits && k > 0;
+  }
+  return AS2D_OK;
+}
+
+// Grows a device buffer of the context that no captured graph holds.
+int grow(as2d_ctx* c, void** p, size_t* cap, size_t bytes) {
+  if (bytes <= *cap) return AS2D_OK;
+  if (*p) {
+    HIP_TRY(c, hipStreamSynchronize(c->stream));
+    c->allocs.erase(std::find(c->allocs.begin(), c->allocs.end(), *p));
+    hipFree(*p);
+    *p = nullptr;
+    *cap = 0;
+  }
+  const int rc = dalloc(c, p, bytes);
+  if (!rc) *cap = bytes;
+  return rc;
+}
+
+// Requests and drafter's logits of a sampling call to the device, before the
+// pass (the rows' order is h_rows'; row r of a request's logits belongs to its
+// row r, so only the rows up to the last one with children are there).
+int upload_sampling(as2d_ctx* c, int n, const int32_t* ks, const int32_t* parents, const as2d_sampling* sampling, bool draft) {
+  const size_t V = c->cfg.vocab;
+  join_op(c);
+  if (draft) {
+    const ReqDesc& last = c->h_reqs[n - 1];
+    const int rc = grow(c, (void**)&c->draft, &c->draft_cap, (size_t)(last.row_start + last.W) * V * 4);
+    if (rc) return rc;
+  }
+  int off = 0;
+  for (int r = 0; r < n; off += ks[r++]) {
+    const as2d_sampling& s = sampling[r];
+    const int row0 = c->h_reqs[r].row_start;
+    const bool has = s.draft_logits && ks[r] > 0;
+    c->h_sreq[r] = SampleReq{s.temperature, s.draft_temperature > 0.0 ? s.draft_temperature : s.temperature, row0, ks[r],
+                             has ? row0 : -1, 0};
+    if (!has) continue;
+    int top = 0;   // last row with children
+    for (int i = 0; i < ks[r]; ++i) top = std::max(top, parents ? parents[off + i] + 1 : i);
+    HIP_TRY(c, hipMemcpyAsync(c->draft + (size_t)row0 * V, s.draft_logits, (size_t)(top + 1) * V * 4, hipMemcpyDefault, c->stream));
+  }
+  HIP_TRY(c, hipMemcpyAsync(c->d_sreq, c->h_sreq, sizeof(SampleReq) * n, hipMemcpyHostToDevice, c->stream));
+  return AS2D_OK;
+}
+
+// Launches of a pass's verification by sampling, from the logits it left.
+int launch_sampling(as2d_ctx* c, int n, int max_k, int max_children, bool draft) {
+  SampleArgs a{};
+  a.vocab = c->cfg.vocab;
+  a.chunks = (a.vocab + kSampleChunk - 1) / kSampleChunk;
+  a.n = n;
+  a.k = max_k;
+  const int rc = grow(c, &c->sample_work, &c->sample_cap, sample_layout(a, max_children, nullptr));
+  if (rc) return rc;
+  sample_layout(a, max_children, (char*)c->sample_work);
+  a.target = c->b.logits;
+  a.draft = draft ? c->draft : nullptr;
+  a.t_stride = a.d_stride = c->cfg.vocab;
+  a.reqs = c->d_sreq;
+  a.rows = c->b.d_rows;
+  a.gate = c->tree.sel;
+  a.tree = c->tree;
+  HIP_TRY(c, launch_sample(a, draft, max_children, c->stream));
+  return AS2D_OK;
+}
+
+int check_rows(as2d_ctx* c, const char* what, const as2d_rows* t) {
+  if (!t || !t->data) return fail(c, AS2D_EINVAL, "%s: null tensor", what);
+  if (t->row_stride < 0 || t->head_stride < 0) return fail(c, AS2D_EINVAL, "%s: negative stride", what);
+  return AS2D_OK;
+}
+
+// Rows from position pos on of one layer of a request's cache.
+PutRows layer_rows(const as2d_ctx* c, int req, int layer, int pos, const as2d_rows* k, const as2d_rows* v) {
+  const as2d_config& g = c->cfg;
+  PutRows a{};
+  a.k = RowsView{k->data, k->row_stride, k->head_stride};
+  a.v = RowsView{v->data, v->row_stride, v->head_stride};
+  a.k_cache = c->kc + (size_t)layer * c->layer_stride;
+  a.v_cache = c->vc + (size_t)layer * c->layer_stride;
+  a.slot_stride = c->slot_stride;
+  a.kv_cap = c->kv_stride;
+  a.slot = req;
+  a.pos0 = pos;
+  a.n_q = g.n_q_heads;
+  a.n_kv = g.n_kv_heads;
+  a.head_dim = g.head_dim;
+  return a;
 }
 
 // Split-K counters a pass of up to `rows` rows may use: one per workgroup
@@ -1063,6 +1278,7 @@ const char* as2d_last_error(const as2d_ctx* c) {
 
 void as2d_free(as2d_ctx* c) {
   if (!c) return;
+  join_op(c);
   if (c->stream) hipStreamSynchronize(c->stream);
   for (void* p : c->allocs) hipFree(p);
   if (c->h_rows) hipHostFree(c->h_rows);
@@ -1070,6 +1286,9 @@ void as2d_free(as2d_ctx* c) {
   if (c->h_out) hipHostFree(c->h_out);
   if (c->h_tok) hipHostFree(c->h_tok);
   if (c->h_margin) hipHostFree(c->h_margin);
+  if (c->tree.host_path) hipHostFree(c->tree.host_path);
+  if (c->h_sreq) hipHostFree(c->h_sreq);
+  if (c->op_ev) hipEventDestroy(c->op_ev);
   for (hipEvent_t e : c->ev_pool) hipEventDestroy(e);
   for (auto& kv : c->graphs) hipGraphExecDestroy(kv.second);
   if (c->own_stream && c->stream) hipStreamDestroy(c->stream);
@@ -1136,6 +1355,7 @@ int as2d_load_weights(const as2d_config* cfg, const void* const* host, int32_t n
     c->own_stream = true;
   }
   if (stream_restricted(c->stream)) return bad(kRestrictedStream);
+  if (hipGetDevice(&c->dev) != hipSuccess) return bad("no device");
   if (H % KE || (nq * d) % KE || F % KE) return bad("inner dimensions must be multiples of the k-step");
 
   // GEMM plans: k-splits depend on the matrix shape only
@@ -1292,6 +1512,12 @@ int as2d_load_weights(const as2d_config* cfg, const void* const* host, int32_t n
   HIP_TRY(c, hipMemsetAsync(c->b.attn_cnt, 0, (size_t)g.max_requests * nq * 2 * 4, c->stream));
   CK(dalloc(c, &c->b.d_reqs, sizeof(ReqDesc) * 2 * g.max_requests));
   CK(dalloc(c, &c->b.d_out, sizeof(StepOut) * g.max_requests));
+  CK(dalloc(c, &c->tree.sel, sizeof(StepOut) * g.max_requests));
+  CK(dalloc(c, &c->tree.path, sizeof(int) * MR));
+  CK(dalloc(c, &c->d_sreq, sizeof(SampleReq) * g.max_requests));
+  CK(dalloc(c, &c->op_rows, sizeof(RowDesc) * kStepRows));
+  CK(dalloc(c, &c->op_req, sizeof(ReqDesc)));
+  HIP_TRY(c, hipEventCreateWithFlags(&c->op_ev, hipEventDisableTiming));
 
   // rotary table, evaluated in double precision: [pos][i] -> (cos, sin)
   {
@@ -1313,9 +1539,11 @@ int as2d_load_weights(const as2d_config* cfg, const void* const* host, int32_t n
   auto pinned = [](auto** p, size_t bytes) { return hipHostMalloc((void**)p, bytes, hipHostMallocCoherent) == hipSuccess; };
   if (!pinned(&c->h_rows, sizeof(RowDesc) * rows) || !pinned(&c->h_reqs, sizeof(ReqDesc) * 2 * g.max_requests) ||
       !pinned(&c->h_out, sizeof(StepOut) * g.max_requests) || !pinned(&c->h_tok, sizeof(int) * MR) ||
-      !pinned(&c->h_margin, sizeof(float) * MR)) {
+      !pinned(&c->h_margin, sizeof(float) * MR) || !pinned(&c->tree.host_path, sizeof(int) * MR) ||
+      !pinned(&c->h_sreq, sizeof(SampleReq) * g.max_requests)) {
     return fail(c, AS2D_ENOMEM, "pinned host buffers");
   }
+  c->tree.host = c->h_out;
   memset(c->h_reqs, 0, sizeof(ReqDesc) * 2 * g.max_requests);
   c->reqs.assign(g.max_requests, ReqState());
   c->exec_mode = env_int("AS2D_EXEC_MODE", AS2D_EXEC_GRAPH);
@@ -1368,7 +1596,7 @@ int as2d_prefill_kv(as2d_ctx* c, int32_t req, const void* audio, int32_t n_audio
       RowDesc rd{};
       rd.token = p < n_audio ? -1 : instr[p - n_audio];
       rd.src = p < n_audio ? p : 0;
-      rd.pos = p;
+      rd.pos = rd.rot = p;
       rd.slot = req;
       rd.cmp = -1;
       c->h_rows[i] = rd;
@@ -1420,6 +1648,7 @@ int as2d_verify_static(as2d_ctx* c, int32_t req, const int32_t* cands, int32_t k
     return fail(c, AS2D_ECAPACITY, "verify_static: the pass needs %zu bytes of static scratch, %zu available (%d keys)",
                 need, cap, c->h_reqs[0].L0 + M);
   hipStream_t s = c->stream;
+  join_op(c);
   // the array keeps the last call's contents: counters must start at zero
   HIP_TRY(c, launch_fill_zero(S.counters, (int)(S.attn_cnt - S.counters) + mr * g.n_q_heads * 2, s));
   const int timing = c->timing;   // no event bracketing here (events are created on first use)
@@ -1438,6 +1667,127 @@ int as2d_verify(as2d_ctx* c, int32_t req, const int32_t* cands, int32_t k, as2d_
 int as2d_decode_one(as2d_ctx* c, int32_t req, as2d_verify_out* out) {
   const int32_t k = 0;
   return as2d_verify_batch(c, 1, &req, nullptr, &k, out);
+}
+
+int as2d_verify_tree_batch(as2d_ctx* c, int32_t n, const int32_t* reqs, const int32_t* cands, const int32_t* parents,
+                           const int32_t* ks, const as2d_sampling* sampling, as2d_verify_out* outs, int32_t* paths) {
+  int M = 0;
+  int rc = assemble_verify(c, n, reqs, cands, ks, outs, kMaxRows, &M);
+  if (rc) return rc;
+  OnDevice on(c->dev);
+  bool draft = false;
+  int max_children = 0, max_k = 0;
+  if ((rc = assemble_tree(c, n, parents, ks, sampling, &max_k, &max_children, &draft))) return rc;
+  if (sampling && (rc = upload_sampling(c, n, ks, parents, sampling, draft))) return rc;
+  const int keep = c->keep_logits;
+  if (sampling) c->keep_logits = 1;   // the pass writes the rows' logits
+  rc = run_forward(c, M, n, n, true, true, true, [&]() -> int {
+    if (sampling) {
+      const int rc = launch_sampling(c, n, max_k, max_children, draft);
+      if (rc) return rc;
+    }
+    const as2d_config& g = c->cfg;
+    MovePath m{c->b.d_reqs + g.max_requests, c->tree.sel, c->tree.path, c->kc, c->vc, c->slot_stride, c->layer_stride,
+               c->kv_stride, g.n_kv_heads, g.head_dim};
+    HIP_TRY(c, launch_move_path(c->bf16, m, g.n_layers, n, c->stream));
+    return AS2D_OK;
+  });
+  c->keep_logits = keep;
+  if (rc) return rc;
+  if (paths) {
+    int off = 0;
+    for (int r = 0; r < n; off += ks[r++])
+      for (int j = 0; j < ks[r]; ++j)
+        paths[off + j] = j < c->h_out[r].accepted && !c->h_out[r].nan_flag ? c->tree.host_path[c->h_reqs[r].row_start + j] : -1;
+  }
+  return commit_verify(c, n, reqs, ks, outs);
+}
+
+int as2d_verify_tree(as2d_ctx* c, int32_t req, const int32_t* cands, const int32_t* parents, int32_t k,
+                     as2d_verify_out* out, int32_t* path) {
+  return as2d_verify_tree_batch(c, 1, &req, cands, parents, &k, nullptr, out, path);
+}
+
+int as2d_verify_sampled(as2d_ctx* c, int32_t req, const int32_t* cands, const int32_t* parents, int32_t k,
+                        const as2d_sampling* sampling, as2d_verify_out* out, int32_t* path) {
+  if (c && !sampling) return fail(c, AS2D_EINVAL, "verify_sampled: null sampling");
+  return as2d_verify_tree_batch(c, 1, &req, cands, parents, &k, sampling, out, path);
+}
+
+int as2d_tree_attention(as2d_ctx* c, int32_t req, int32_t layer, int32_t n_rows, const int32_t* parents,
+                        const as2d_rows* q, const as2d_rows* k, const as2d_rows* v, const as2d_rows* out,
+                        void* hip_stream) {
+  int rc = check_req(c, req);
+  if (rc) return rc;
+  const as2d_config& g = c->cfg;
+  const ReqState& st = c->reqs[req];
+  if (!st.active) return fail(c, AS2D_ESTATE, "tree_attention: request %d has not been prefilled", req);
+  if (layer < 0 || layer >= g.n_layers) return fail(c, AS2D_EINVAL, "tree_attention: layer %d out of range", layer);
+  if (n_rows < 1 || n_rows > kStepRows) return fail(c, AS2D_EINVAL, "tree_attention: %d rows outside [1, %d]", n_rows, kStepRows);
+  if (st.kv_len + n_rows > g.max_kv_len)
+    return fail(c, AS2D_ECAPACITY, "tree_attention: request %d needs %d positions > %d", req, st.kv_len + n_rows, g.max_kv_len);
+  if ((rc = check_rows(c, "tree_attention", q)) || (rc = check_rows(c, "tree_attention", k)) ||
+      (rc = check_rows(c, "tree_attention", v)) || (rc = check_rows(c, "tree_attention", out)))
+    return rc;
+  PutRows a = layer_rows(c, req, layer, st.kv_len, k, v);
+  if ((rc = tree_masks(c, "tree_attention", parents, n_rows - 1, a.mask, nullptr, nullptr))) return rc;
+  OnDevice on(c->dev);
+  hipStream_t s = (hipStream_t)hip_stream;
+  if ((rc = begin_op(c, s))) return rc;
+  a.q = RowsView{q->data, q->row_stride, q->head_stride};
+  a.q_out = c->b.q;
+  a.rows = c->op_rows;
+  a.req = c->op_req;
+  HIP_TRY(c, launch_put_rows(c->bf16, c->bf16, a, n_rows, s));
+  const ReqDesc rq{0, n_rows, st.kv_len, req};
+  const int blocks = (st.kv_len + n_rows + kAttnBlock - 1) / kAttnBlock, spans = (blocks + kAttnSpan - 1) / kAttnSpan;
+  AttnArgs t{};
+  t.q = c->b.q;
+  t.k_cache = a.k_cache;
+  t.v_cache = a.v_cache;
+  t.slot_stride = c->slot_stride;
+  t.kv_cap = c->kv_stride;
+  t.rows = c->op_rows;
+  t.reqs = c->op_req;
+  t.n_q = g.n_q_heads;
+  t.n_kv = g.n_kv_heads;
+  t.head_dim = g.head_dim;
+  t.scale = attn_scale(g.head_dim);
+  t.pacc = c->b.pacc;
+  t.pml = c->b.pml;
+  t.part_spans = spans;
+  t.merge_last = merge_last(spans);
+  t.attn_cnt = c->b.attn_cnt;
+  t.M = n_rows;
+  t.tree = 1;
+  t.rows_out = out->data;
+  t.rows_out_row = out->row_stride;
+  t.rows_out_head = out->head_stride;
+  t.wave_tiles = wave_tiles(c, n_rows, &rq, 1, spans);
+  t.attn_rt = c->attn_rt;
+  t.cus = c->grid_cus;
+  HIP_TRY(c, launch_attention(c->bf16, t, 1, blocks, false, s));
+  return AS2D_OK;
+}
+
+int as2d_write_kv(as2d_ctx* c, int32_t req, int32_t layer, int32_t pos, int32_t n_tok, int32_t dtype,
+                  const as2d_rows* k, const as2d_rows* v, void* hip_stream) {
+  int rc = check_req(c, req);
+  if (rc) return rc;
+  const as2d_config& g = c->cfg;
+  const ReqState& st = c->reqs[req];
+  if (!st.active) return fail(c, AS2D_ESTATE, "write_kv: request %d has not been prefilled", req);
+  if (layer < 0 || layer >= g.n_layers || (dtype != AS2D_F32 && dtype != AS2D_BF16))
+    return fail(c, AS2D_EINVAL, "write_kv: bad layer or type");
+  if (pos < 0 || n_tok < 0 || pos > st.kv_len || n_tok > st.kv_len - pos)
+    return fail(c, AS2D_EINVAL, "write_kv: positions [%d, %d + %d) outside the request's %d", pos, pos, n_tok, st.kv_len);
+  if ((rc = check_rows(c, "write_kv", k)) || (rc = check_rows(c, "write_kv", v))) return rc;
+  if (!n_tok) return AS2D_OK;
+  OnDevice on(c->dev);
+  hipStream_t s = (hipStream_t)hip_stream;
+  if ((rc = begin_op(c, s))) return rc;
+  HIP_TRY(c, launch_put_rows(c->bf16, dtype == AS2D_BF16, layer_rows(c, req, layer, pos, k, v), n_tok, s));
+  return AS2D_OK;
 }
 
 int as2d_set_keep_logits(as2d_ctx* c, int32_t on) {
@@ -1515,6 +1865,7 @@ int as2d_read_kv(as2d_ctx* c, int32_t req, int32_t layer, void* host_k, void* ho
   const as2d_config& g = c->cfg;
   if (layer < 0 || layer >= g.n_layers || n_tok < 0 || n_tok > g.max_kv_len || !host_k || !host_v)
     return fail(c, AS2D_EINVAL, "read_kv: bad arguments");
+  join_op(c);
   HIP_TRY(c, hipStreamSynchronize(c->stream));
   const size_t d = (size_t)g.head_dim, cap = (size_t)c->kv_stride;
   float* ok = static_cast<float*>(host_k);
@@ -1556,6 +1907,7 @@ int as2d_read_kv(as2d_ctx* c, int32_t req, int32_t layer, void* host_k, void* ho
 int as2d_set_stream(as2d_ctx* c, void* hip_stream) {
   if (!c) return AS2D_EINVAL;
   if (hip_stream && stream_restricted((hipStream_t)hip_stream)) return fail(c, AS2D_EINVAL, "set_stream: %s", kRestrictedStream);
+  join_op(c);
   HIP_TRY(c, hipStreamSynchronize(c->stream));
   drop_launch_state(c);
   if (c->own_stream) {
@@ -1665,9 +2017,10 @@ int as2d_time_gemm(as2d_ctx* c, int32_t which, int32_t rows, int32_t reps, doubl
     return c ? fail(c, AS2D_EINVAL, "time_gemm: bad arguments") : AS2D_EINVAL;
   const as2d_config& g = c->cfg;
   hipStream_t s = c->stream;
+  join_op(c);
   // rows describe positions 0..rows-1 of slot 0: only the QKV epilogue reads
   // them (cache rows it overwrites are in bounds; their contents are garbage)
-  for (int i = 0; i < rows; ++i) c->h_rows[i] = RowDesc{0, 0, std::min(i, g.max_kv_len - 1), 0, -1, {0, 0, 0}};
+  for (int i = 0; i < rows; ++i) c->h_rows[i] = RowDesc{0, 0, std::min(i, g.max_kv_len - 1), 0, -1, std::min(i, g.max_kv_len - 1), 0, 0.f};
   HIP_TRY(c, hipMemcpyAsync(c->b.d_rows, c->h_rows, sizeof(RowDesc) * rows, hipMemcpyHostToDevice, s));
   hipEvent_t e0 = ev_get(c, 1000), e1 = ev_get(c, 1001);
   if (!e0 || !e1) return fail(c, AS2D_EHIP, "time_gemm: events");

@@ -6,7 +6,8 @@
 // g = floor(h n_kv / n_q).  Keys are taken in spans of kAttnSpanKeys = 128 at
 // absolute positions, and a span in four chunks of kAttnChunk = 32 keys (one
 // per wave); chunk c of span sp holds keys [128 sp + 32 c, 128 sp + 32 c + 32)
-// up to pos:
+// up to pos (in a tree of candidates, TREE: up to the committed length, and the
+// request's rows in the row's mask; a hidden key counts as one after pos):
 //   s_j   = (q . k_j) * scale, a matrix-core product: for bf16 models q and
 //           k are split into bf16 pairs (hi = bf16(x), lo = bf16(x - hi))
 //           and s = q_hi k_hi + q_hi k_lo + q_lo k_hi over 32-wide k-steps;
@@ -309,6 +310,12 @@ __device__ __forceinline__ Op2 attn_v_operand(const AttnRaw<BF, D>& r, int t, in
   return o;
 }
 
+// Whether a tree's row at cache row pos sees the key: a committed one, or a
+// row of its mask (no bit past the row is set; pos - L0 < 32).
+__device__ __forceinline__ bool tree_sees(uint32_t mask, int key, int L0, int pos) {
+  return key < L0 || (key <= pos && (mask >> ((key - L0) & 31) & 1u));
+}
+
 // Running attention state of this lane's rows (16 rt + 4 (lane / 16) + i)
 // and dimensions (16 (w DTW + t) + lane % 16).
 template <int RT, int DTW> struct AttnState {
@@ -352,7 +359,7 @@ __device__ __forceinline__ void attn_state_merge(AttnState<RT, DTW>& st, const f
 struct NoOp {
   __device__ void operator()() const {}
 };
-template <bool BF, int D, int RT, class PreV = NoOp>
+template <bool BF, int D, int RT, bool TREE = false, class PreV = NoOp>
 __device__ __forceinline__ void attn_span_chunks(const AttnArgs& p, const ReqDesc& rq, const AttnRows& rows, int sp,
                                                  const Op2 (&q)[RT][D / AttnFmt<BF>::KE], const AttnRaw<BF, D>& raw,
                                                  unsigned char* smem, PreV pre_v = PreV{}) {
@@ -376,13 +383,20 @@ __device__ __forceinline__ void attn_span_chunks(const AttnArgs& p, const ReqDes
   for (int rt = 0; rt < RT; ++rt) {
     // s transposed: lane l holds keys kc + 16 kt + 4 (l / 16) + i of block row 16 rt + l % 16
     const int pos = rq.L0 + rows.row(16 * rt + lr);
+    // a chunk that reaches the tree's rows (wave-uniform); the other chunks' keys all precede them
+    const bool in_tree = TREE && kc + kAttnChunk > rq.L0;
+    const uint32_t mask = in_tree ? ldg(&p.rows[rq.row_start + pos - rq.L0].mask) : 0;
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       f4 acc = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) acc = mma3<BF>(raw.k[kt][ks], q[rt][ks], acc);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[rt][kt][i] = kc + 16 * kt + 4 * lg + i <= pos ? acc[i] * p.scale : -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        const int key = kc + 16 * kt + 4 * lg + i;
+        const bool sees = in_tree ? tree_sees(mask, key, rq.L0, pos) : key <= pos;
+        s[rt][kt][i] = sees ? acc[i] * p.scale : -INFINITY;
+      }
     }
   }
   pre_v();   // a caller that fetches the values only now (the keys' registers are free)
@@ -478,11 +492,11 @@ __device__ __forceinline__ void attn_merge_chunks(unsigned char* smem, AttnState
   }
 }
 
-template <bool BF, int D, int RT>
+template <bool BF, int D, int RT, bool TREE = false>
 __device__ __forceinline__ void attn_span_state(const AttnArgs& p, const ReqDesc& rq, const AttnRows& rows, int sp,
                                                 const Op2 (&q)[RT][D / AttnFmt<BF>::KE], const AttnRaw<BF, D>& raw,
                                                 unsigned char* smem, AttnState<RT, D / 64>& st) {
-  attn_span_chunks<BF, D, RT>(p, rq, rows, sp, q, raw, smem);
+  attn_span_chunks<BF, D, RT, TREE>(p, rq, rows, sp, q, raw, smem);
   attn_merge_chunks<BF, D, RT>(smem, st);
 }
 
@@ -523,12 +537,40 @@ __device__ __forceinline__ void attn_store_span(const AttnArgs& p, const ReqDesc
     }
 }
 
+// The attention output of a row: N consecutive dimensions from n = h D + dim.
+// A tree pass may ask for rows of the model's type (rows_out, any strides and
+// element alignment); the next GEMM takes activation planes.
+template <bool BF, int D, bool OUT_COH, bool TREE, int N>
+__device__ __forceinline__ void attn_store_out(const AttnArgs& p, int row, int n, const float* o) {
+  if constexpr (TREE)
+    if (p.rows_out) {
+      const size_t at = (size_t)row * p.rows_out_row + (size_t)(n / D) * p.rows_out_head + n % D;
+      if constexpr (BF) {
+        typedef uint16_t run __attribute__((ext_vector_type(N), aligned(2)));
+        run v;
+#pragma unroll
+        for (int t = 0; t < N; ++t) v[t] = f2bf(o[t]);
+        *gmem(reinterpret_cast<run*>(static_cast<uint16_t*>(p.rows_out) + at)) = v;
+      } else {
+        typedef float run __attribute__((ext_vector_type(N), aligned(4)));
+        run v;
+#pragma unroll
+        for (int t = 0; t < N; ++t) v[t] = o[t];
+        *gmem(reinterpret_cast<run*>(static_cast<float*>(p.rows_out) + at)) = v;
+      }
+      return;
+    }
+  const size_t e = frag_index<BF>(row, n, p.n_q * D);
+  if constexpr (N == 1) store_act<BF, OUT_COH>(p.out, p.out_plane, e, o[0]);
+  else store_act_run<BF, OUT_COH, N>(p.out, p.out_plane, e, o);
+}
+
 // Row r of request rq, head h: its span states (stored by attn_store_span,
 // read with agent-scope loads) merged in ascending order, by one quarter
 // wave (lane l % 16 holds dimensions [DQ (l % 16), DQ (l % 16) + DQ),
 // DQ = D / 16); writes the attention output planes (OUT_COH: with
 // agent-scope stores).
-template <bool BF, int D, bool OUT_COH>
+template <bool BF, int D, bool OUT_COH, bool TREE = false>
 __device__ __forceinline__ void attn_merge_row(const AttnArgs& p, const ReqDesc& rq, int r, int h) {
   constexpr int DQ = D / 16;   // dimensions per lane
   constexpr int kB = 8;        // spans whose loads are in flight together
@@ -589,7 +631,7 @@ __device__ __forceinline__ void attn_merge_row(const AttnArgs& p, const ReqDesc&
   float o[DQ];
 #pragma unroll
   for (int t = 0; t < DQ; ++t) o[t] = A[t] / L;
-  store_act_run<BF, OUT_COH, DQ>(p.out, p.out_plane, frag_index<BF>(row, h * D + DQ * ql, p.n_q * D), o);
+  attn_store_out<BF, D, OUT_COH, TREE, DQ>(p, row, h * D + DQ * ql, o);
 }
 
 // Row i of request rq, head h, by one wave: the same fold as attn_merge_row
@@ -600,7 +642,7 @@ __device__ __forceinline__ void attn_merge_row(const AttnArgs& p, const ReqDesc&
 // running maximum before span s is the maximum of m over spans 0 .. s - 1,
 // which a prefix scan gives exactly (fmax rounds nothing).  The states were
 // stored by an earlier kernel; the output planes are read by a later one.
-template <bool BF, int D>
+template <bool BF, int D, bool TREE = false>
 __device__ __forceinline__ void attn_merge_wave(const AttnArgs& p, const ReqDesc& rq, int i, int h) {
 #pragma clang fp contract(off)
   constexpr int DL = D / 64;   // dimensions per lane
@@ -673,9 +715,7 @@ __device__ __forceinline__ void attn_merge_wave(const AttnArgs& p, const ReqDesc
   float o[DL];
 #pragma unroll
   for (int t = 0; t < DL; ++t) o[t] = A[t] / L;
-  const size_t e = frag_index<BF>(row, h * D + DL * lane, p.n_q * D);
-  if constexpr (DL == 2) store_act_run<BF, false, 2>(p.out, p.out_plane, e, o);
-  else store_act<BF, false>(p.out, p.out_plane, e, o[0]);
+  attn_store_out<BF, D, false, TREE, DL>(p, row, h * D + DL * lane, o);
 }
 
 }  // namespace as2d

@@ -18,6 +18,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "plan.h"
 
 namespace as2d {
@@ -47,11 +49,17 @@ enum PackMap {
 struct RowDesc {
   int32_t token;   // embedding row, or -1: take audio staging row `src`
   int32_t src;     // audio staging row
-  int32_t pos;     // position (also the KV cache row it writes)
+  int32_t pos;     // KV cache row it writes
   int32_t slot;    // KV cache slot of its request
   int32_t cmp;     // candidate its greedy token is compared with (-1: none)
-  int32_t pad[3];
+  int32_t rot;     // rotary position: pos, or in a tree the committed positions and the row's depth
+  uint32_t mask;   // passes over trees: bit t is set where row t of the request is an ancestor or the row itself
+  float u;         // passes that sample: the row's random number (row 0: the final token's)
 };
+
+// Row of a tree's row i >= 1 that its candidate follows: the highest ancestor
+// in its mask.
+__host__ __device__ inline int parent_row(uint32_t mask, int i) { return 31 - __builtin_clz(mask ^ (1u << i)); }
 
 // One request of a forward pass: rows [row_start, row_start + W).
 struct ReqDesc {
@@ -176,6 +184,9 @@ struct AttnArgs {
   void* out;             // planes [rows][n_q*d]
   long long out_plane;
   int M;
+  int tree;              // verification passes: rows see the committed keys and the request's rows in their mask
+  void* rows_out;        // tree: the output as rows of the model's type instead of the planes
+  long long rows_out_row, rows_out_head;   // its strides, in elements
   int wave_tiles;        // verification passes of bf16 models: a row tile per wave (attn_spans_wide_kernel)
   int attn_rt;           // row tiles per block of the verification kernel (0: chosen per launch)
   int cus;               // compute units the verification kernels may fill (the CU budget)
@@ -265,6 +276,116 @@ hipError_t launch_attn_spans(const AttnArgs& a, int n_reqs, int grid, hipStream_
 hipError_t launch_finish(const RowDesc* rows, const ReqDesc* reqs, int n_reqs, int n_rows,
                          const float* amax_val, const float* amax_val2, const int* amax_idx, int n_pairs,
                          int* row_tok, int* row_bad, int* counters, const HostOut& out, hipStream_t s);
+
+// Passes over trees (tree.hip).  Rows [n][heads][head_dim] of a device
+// tensor, dimensions adjacent, strides in elements.
+struct RowsView {
+  const void* data;
+  long long row_stride, head_stride;
+};
+// Rows into cache rows pos0 .. of one layer and, with q_out, the queries and
+// descriptors of a tree attention.
+struct PutRows {
+  RowsView q, k, v;
+  float *k_cache, *v_cache;   // this layer
+  long long slot_stride;
+  int kv_cap, slot, pos0, n_q, n_kv, head_dim;
+  float* q_out;               // [n][n_q * head_dim], or null: only the cache is written
+  RowDesc* rows;
+  ReqDesc* req;
+  uint32_t mask[32];
+};
+// src_bf16: the type of q, k and v.
+hipError_t launch_put_rows(bool bf16, bool src_bf16, const PutRows& a, int n, hipStream_t s);
+
+// Outcome of a pass over trees, on the device and in pinned host memory:
+// per request (accepted -1: non-finite), and the accepted candidates from
+// the request's first row on.
+struct TreeOut {
+  StepOut* sel;
+  int* path;
+  StepOut* host;
+  int* host_path;
+};
+hipError_t launch_tree_walk(const RowDesc* rows, const ReqDesc* reqs, int n_reqs, const int* row_tok, const int* row_bad,
+                            const TreeOut& out, hipStream_t s);
+
+// The accepted paths' cache rows, every layer.
+struct MovePath {
+  const ReqDesc* reqs;
+  const StepOut* sel;
+  const int* path;
+  float *k_cache, *v_cache;   // the first layer
+  long long slot_stride, layer_stride;
+  int kv_cap, n_kv, head_dim;
+};
+hipError_t launch_move_path(bool bf16, const MovePath& a, int n_layers, int n_reqs, hipStream_t s);
+
+// Verification by sampling (sample.hip).  A request of a pass:
+struct SampleReq {
+  double temp, draft_temp;
+  int32_t row0, k;             // first row of the logits, candidates
+  int32_t draft_row0;          // first row of the drafter's logits, -1: none
+  int32_t pad;
+};
+struct SamplePart {            // one chunk of a row: maximum, sum of 2^((x - max) c), whether a value is NaN or +inf
+  double sum;
+  float max;
+  int bad;
+};
+struct SampleDecision {
+  int bad, accepted, node, n_gone;   // node: the row whose distribution gives the token
+  double u, cut;                     // its random number; multiples of the drafter's distribution taken off
+  double c, log_sum, dc, dlog_sum;   // log2(e) / temperature and log2 of the sum, target and drafter
+  float max, dmax;
+  int draft, pad;
+  int gone[32];                      // rejected candidates of the node (no drafter)
+};
+struct SampleArgs {
+  const void* target;          // [rows][vocab], float32 or bf16
+  const void* draft;           // the same of the drafter (row r: what row r's children were drawn from), or null
+  long long t_stride, d_stride;
+  int n, k, vocab, chunks;     // k: most candidates of a request; chunks of kSampleChunk logits
+  int bf16;
+  // a pass of the verification step: requests and rows of its descriptors
+  const SampleReq* reqs;
+  const RowDesc* rows;
+  const StepOut* gate;         // nan_flag: the request is not decided
+  TreeOut tree;
+  // a batch of device tensors (reqs null): request r has rows r (k + 1) ..
+  const int* cands;            // [n][k]
+  const int* ks;               // [n] or null: k each
+  const float* uniforms;       // [n][k + 1]
+  const float* temps;          // [n] or null: temp
+  double temp, draft_temp;     // draft_temp 0: the target's
+  signed char parent[32];      // row that row i follows
+  int *accepted, *path, *token;   // [n], [n][k], [n]
+  float* logp;                 // [n][k + 1] or null
+  // workspace
+  SamplePart* part;            // [n][2][k + 1][chunks]
+  double* stage;               // [max_children - 1][n][k + 1][chunks]
+  double* cut;                 // [max_children][n][k + 1]
+  double* left;                // [n][chunks]
+  SampleDecision* dec;         // [n]
+};
+constexpr int kSampleChunk = 4096;
+// Workspace of a (n, k, chunks set): its bytes; with base, points a's arrays into it.
+inline size_t sample_layout(SampleArgs& a, int max_children, char* base) {
+  size_t off = 0;
+  const auto take = [&](auto** p, size_t n) {
+    *p = reinterpret_cast<std::remove_reference_t<decltype(**p)>*>(base + off);
+    off += (n * sizeof(**p) + 255) / 256 * 256;
+  };
+  const size_t rows = (size_t)a.n * (a.k + 1), stages = max_children > 1 ? max_children - 1 : 0;
+  take(&a.part, 2 * rows * a.chunks);
+  take(&a.stage, stages * rows * a.chunks);
+  take(&a.cut, stages * rows);
+  take(&a.left, (size_t)a.n * a.chunks);
+  take(&a.dec, a.n);
+  return off;
+}
+// draft: some request has a drafter's logits; max_children: most children of a row.
+hipError_t launch_sample(const SampleArgs& a, bool draft, int max_children, hipStream_t s);
 
 // Zeroes n ints (a kernel, not a memset, so that it may be captured).
 hipError_t launch_fill_zero(int* p, int n, hipStream_t s);

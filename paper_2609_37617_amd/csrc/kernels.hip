@@ -88,7 +88,8 @@ __global__ __launch_bounds__(256) void embed_kernel(const RowDesc* rows, const P
   if (put.rows) {
     const u32x4* src = reinterpret_cast<const u32x4*>(rows + m);
     const u32x4 a = __builtin_nontemporal_load(src), b = __builtin_nontemporal_load(src + 1);
-    rd = RowDesc{(int32_t)a.x, (int32_t)a.y, (int32_t)a.z, (int32_t)a.w, (int32_t)b.x, {0, 0, 0}};
+    rd = RowDesc{(int32_t)a.x, (int32_t)a.y, (int32_t)a.z, (int32_t)a.w, (int32_t)b.x,
+                 (int32_t)b.y, b.z, __uint_as_float(b.w)};
     if (threadIdx.x == 0) put.rows[m] = rd;
     if (m == 0)
       for (int i = threadIdx.x; i < put.n_att + put.n_fin; i += 256) {
@@ -318,7 +319,7 @@ hipError_t launch_gemm(bool bf16, int amode, int epi, const GemmArgs& a, hipStre
 // The items of a launch with blocks of RT row tiles.  LOWREG (RT = 1): a
 // workgroup within half the register file (two per compute unit), one span
 // buffer, the values fetched once the span's scores are formed.
-template <bool BF, int D, int RT, bool LOWREG = false>
+template <bool BF, int D, int RT, bool TREE, bool LOWREG = false>
 __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, unsigned char* smem) {
   static_assert(!LOWREG || RT == 1, "one row tile");
   constexpr int KS = D / AttnFmt<BF>::KE;
@@ -354,7 +355,7 @@ __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, 
     attn_load_q<BF, D, RT>(p, rq, rows, q);
     auto run = [&](int sp, const AttnRaw<BF, D>& raw) {
       AttnState<RT, D / 64> state;
-      attn_span_state<BF, D, RT>(p, rq, rows, sp, q, raw, smem, state);
+      attn_span_state<BF, D, RT, TREE>(p, rq, rows, sp, q, raw, smem, state);
       attn_store_span<D, RT>(p, rq, rows, sp, state);
       lds_sync();   // the LDS is written again next (a prefetch stays in flight)
     };
@@ -363,7 +364,7 @@ __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, 
       // span's keys, requested right after the span's values
       for (int sp = sp0; sp < sp1; ++sp) {
         AttnState<1, D / 64> state;
-        attn_span_chunks<BF, D, 1>(p, rq, rows, sp, q, ka, smem, [&] {
+        attn_span_chunks<BF, D, 1, TREE>(p, rq, rows, sp, q, ka, smem, [&] {
           attn_fetch_v<BF, D>(p, rq, g, sp, ka);
           if (sp + 1 < sp1) attn_fetch_k<BF, D>(p, rq, g, sp + 1, ka);
         });
@@ -403,7 +404,7 @@ __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, 
       if (s_last) {
         if (threadIdx.x == 0) st<true>(cnt, 0);   // ready for the next launch
         const int nv = min(BR, rows.n - rows.u0);
-        for (int k = threadIdx.x >> 4; k < nv; k += 16) attn_merge_row<BF, D, false>(p, rq, rows.row(k), rows.head(k));
+        for (int k = threadIdx.x >> 4; k < nv; k += 16) attn_merge_row<BF, D, false, TREE>(p, rq, rows.row(k), rows.head(k));
       }
       __syncthreads();   // s_last is reused by the next item
     }
@@ -415,7 +416,7 @@ __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, 
 // a third (requests of few rows: the second tile would be padding); else
 // of two (half the reads of the keys and values per row, fewer runs of
 // spans per workgroup).  An attn_rt of 1 or 2 fixes it.
-template <bool BF, int D>
+template <bool BF, int D, bool TREE>
 __global__ __launch_bounds__(256) void attn_group_kernel(const AttnArgs p, int n_reqs) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int rt = p.attn_rt;
@@ -432,20 +433,20 @@ __global__ __launch_bounds__(256) void attn_group_kernel(const AttnArgs p, int n
     const int n1 = n_items(16), n2 = n_items(32);
     rt = n1 <= (int)gridDim.x || 2 * n1 < 3 * n2 ? 1 : 2;
   }
-  if (rt == 1) attn_group_items<BF, D, 1>(p, n_reqs, smem);
-  else attn_group_items<BF, D, 2>(p, n_reqs, smem);
+  if (rt == 1) attn_group_items<BF, D, 1, TREE>(p, n_reqs, smem);
+  else attn_group_items<BF, D, 2, TREE>(p, n_reqs, smem);
 }
 
 // Slots whose one-tile items outnumber the compute units: one-tile blocks
 // on two workgroups per compute unit, each overlapping the other's waits.
-template <bool BF, int D>
+template <bool BF, int D, bool TREE>
 __global__ __launch_bounds__(256, 2) void attn_group2_kernel(const AttnArgs p, int n_reqs) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  attn_group_items<BF, D, 1, true>(p, n_reqs, smem);
+  attn_group_items<BF, D, 1, TREE, true>(p, n_reqs, smem);
 }
 
 // One wave per (request row, query head), heads of a row adjacent.
-template <bool BF, int D>
+template <bool BF, int D, bool TREE>
 __global__ __launch_bounds__(64) void attn_merge_kernel(const AttnArgs p, int n_reqs) {
   int u = blockIdx.x, r = 0;
   if (n_reqs > 1) r = find_request(p.reqs, n_reqs, u, [&](const ReqDesc& q) { return q.W * p.n_q; });
@@ -453,7 +454,7 @@ __global__ __launch_bounds__(64) void attn_merge_kernel(const AttnArgs p, int n_
   const ReqDesc rq = load_invariant(p.reqs + r);
   if (u >= rq.W * p.n_q) return;
   const int i = u / p.n_q;
-  attn_merge_wave<BF, D>(p, rq, i, u - i * p.n_q);
+  attn_merge_wave<BF, D, TREE>(p, rq, i, u - i * p.n_q);
 }
 
 // Prefill attention of float32 models (bf16: attn_prefill.hip): one workgroup
@@ -544,11 +545,11 @@ __global__ __launch_bounds__(512) void attn_prefill_kernel(const AttnArgs p) {
   }
 }
 
-template <bool BF, int D>
+template <bool BF, int D, bool TREE>
 static hipError_t attn_dispatch(const AttnArgs& a, int n_reqs, int max_blocks, bool prefill, hipStream_t s) {
   if (max_blocks > kMaxBlocks || n_reqs < 1) return hipErrorInvalidValue;
   if (prefill) {
-    if (n_reqs != 1) return hipErrorInvalidValue;
+    if (n_reqs != 1 || TREE) return hipErrorInvalidValue;
     if constexpr (BF) return launch_attn_prefill(a, s);
     else attn_prefill_kernel<D><<<dim3(a.n_q, (a.M + 15) / 16), 512, attn_prefill_lds_bytes<D>(), s>>>(a);
     return hipGetLastError();
@@ -565,14 +566,14 @@ static hipError_t attn_dispatch(const AttnArgs& a, int n_reqs, int max_blocks, b
     if (e != hipSuccess) return e;
   } else if (items > cus && a.attn_rt == 0) {
     const int grid2 = (int)std::min<long long>(2 * cus, (items + 7) / 8 * 8);
-    attn_group2_kernel<BF, D><<<grid2, 256, attn_span_lds_bytes<BF, D, 1>(), s>>>(a, n_reqs);
+    attn_group2_kernel<BF, D, TREE><<<grid2, 256, attn_span_lds_bytes<BF, D, 1>(), s>>>(a, n_reqs);
   } else {
     const int grid = (int)std::min<long long>(cus, (items + 7) / 8 * 8);
-    attn_group_kernel<BF, D><<<grid, 256, attn_span_lds_bytes<BF, D, 2>(), s>>>(a, n_reqs);
+    attn_group_kernel<BF, D, TREE><<<grid, 256, attn_span_lds_bytes<BF, D, 2>(), s>>>(a, n_reqs);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.merge_last) return e;
-  attn_merge_kernel<BF, D><<<a.M * a.n_q, 64, 0, s>>>(a, n_reqs);
+  attn_merge_kernel<BF, D, TREE><<<a.M * a.n_q, 64, 0, s>>>(a, n_reqs);
   return hipGetLastError();
 }
 
@@ -614,7 +615,9 @@ static hipError_t prepare_staged() {
 template <bool BF, int D>
 static hipError_t prepare_attention() {
   auto allow = [](const void* k, int bytes) { return hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-  hipError_t e = allow(reinterpret_cast<const void*>(&attn_group_kernel<BF, D>), attn_span_lds_bytes<BF, D, 2>());
+  hipError_t e = allow(reinterpret_cast<const void*>(&attn_group_kernel<BF, D, false>), attn_span_lds_bytes<BF, D, 2>());
+  if (e == hipSuccess)
+    e = allow(reinterpret_cast<const void*>(&attn_group_kernel<BF, D, true>), attn_span_lds_bytes<BF, D, 2>());
   if constexpr (!BF)
     if (e == hipSuccess)
       e = allow(reinterpret_cast<const void*>(&attn_prefill_kernel<D>), attn_prefill_lds_bytes<D>());
@@ -641,10 +644,11 @@ hipError_t prepare_kernels() {
 }
 
 hipError_t launch_attention(bool bf16, const AttnArgs& a, int n_reqs, int max_blocks, bool prefill, hipStream_t s) {
-  if (a.head_dim == 128) return bf16 ? attn_dispatch<true, 128>(a, n_reqs, max_blocks, prefill, s)
-                                     : attn_dispatch<false, 128>(a, n_reqs, max_blocks, prefill, s);
-  if (a.head_dim == 64) return bf16 ? attn_dispatch<true, 64>(a, n_reqs, max_blocks, prefill, s)
-                                    : attn_dispatch<false, 64>(a, n_reqs, max_blocks, prefill, s);
+#define AS2D_A(bf, dim, tr) \
+  if (bf16 == bf && a.head_dim == dim && (a.tree != 0) == tr) return attn_dispatch<bf, dim, tr>(a, n_reqs, max_blocks, prefill, s);
+  AS2D_A(true, 128, false) AS2D_A(true, 64, false) AS2D_A(false, 128, false) AS2D_A(false, 64, false)
+  AS2D_A(true, 128, true) AS2D_A(true, 64, true) AS2D_A(false, 128, true) AS2D_A(false, 64, true)
+#undef AS2D_A
   return hipErrorInvalidValue;
 }
 

@@ -159,8 +159,8 @@ __device__ __forceinline__ void epilogue_rows(const GemmArgs& p, float* F, int f
       if (head < p.n_q + p.n_kv) {
         const int pn = j ? n - half : n + half;
         const float partner = Fr[c ^ 16] + (p.bias ? ldg(p.bias + pn) : 0.0f);
-        const float cs = ldg(p.rope_cs + ((size_t)rd.pos * half + i) * 2);
-        const float sn = ldg(p.rope_cs + ((size_t)rd.pos * half + i) * 2 + 1);
+        const float cs = ldg(p.rope_cs + ((size_t)rd.rot * half + i) * 2);
+        const float sn = ldg(p.rope_cs + ((size_t)rd.rot * half + i) * 2 + 1);
         v = rope(v, j == 0 ? -partner : partner, cs, sn);
         if (head < p.n_q) {
           st<COH>(p.q_out + (size_t)m * p.n_q * d + n, v);
@@ -657,7 +657,7 @@ template <bool BF, int MT, int EPI> struct UnitEpi {
   static constexpr int NE = 2 * MT;
   float c0 = 0.f, c1 = 0.f;      // column: gain, or bias and the partner's bias
   float x[NE];                   // residual
-  int pos[NE], slot[NE];         // cache row and slot
+  int pos[NE], slot[NE], rot[NE];   // cache row and slot, rotary position
   float cs[NE], sn[NE];          // rotation
   int pair = -1;
 
@@ -689,6 +689,7 @@ template <bool BF, int MT, int EPI> struct UnitEpi {
         const RowDesc* r = p.rows + min(row_of(e), M - 1);
         pos[e] = ldg(&r->pos);
         slot[e] = ldg(&r->slot);
+        rot[e] = ldg(&r->rot);
       }
     } else {
       const int n = pair * kPairCols + (threadIdx.x & 31);
@@ -702,7 +703,7 @@ template <bool BF, int MT, int EPI> struct UnitEpi {
       const Col k = col(p);
 #pragma unroll
       for (int e = 0; e < NE; ++e) {
-        const float2 a = ldg(reinterpret_cast<const float2*>(p.rope_cs) + (size_t)pos[e] * (p.head_dim >> 1) + k.i);
+        const float2 a = ldg(reinterpret_cast<const float2*>(p.rope_cs) + (size_t)rot[e] * (p.head_dim >> 1) + k.i);
         cs[e] = a.x;
         sn[e] = a.y;
       }

@@ -176,12 +176,13 @@ __device__ __forceinline__ void wide_epilogue(const GemmArgs& p, float* F, int p
     const int pair = pair0 + (u >> 1), head = pair / ppd, i0 = 16 * (pair - head * ppd) + (u & 1) * 8;
     const bool rotated = head < p.n_q + p.n_kv;
     const int n = head * d + i0;
-    int pos[NR], slot[NR];
+    int pos[NR], slot[NR], rot[NR];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       const RowDesc* r = p.rows + min(r0 + rr + RP * i, r1 - 1);
       pos[i] = ldg(&r->pos);
       slot[i] = ldg(&r->slot);
+      rot[i] = ldg(&r->rot);
     }
     float b0[8] = {}, b1[8] = {};
     if (p.bias) {
@@ -195,7 +196,7 @@ __device__ __forceinline__ void wide_epilogue(const GemmArgs& p, float* F, int p
 #pragma unroll
     for (int i = 0; i < NR; ++i)
       if (rotated) {
-        const float* q = p.rope_cs + ((size_t)pos[i] * half + i0) * 2;
+        const float* q = p.rope_cs + ((size_t)rot[i] * half + i0) * 2;
         load8(q, cs[i][0]);
         load8(q + 8, cs[i][1]);
       }

@@ -1,0 +1,299 @@
+"""Verification by sampling on the GPU (as2d_sampler_*), against the float64
+oracle: accepted paths and tokens equal, log-probabilities to float32."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import trees                     # noqa: E402
+from paper_2609_37617_amd import as2d        # noqa: E402
+from tests.harness import ensure_built       # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+# logp is one rounding to float32 (2^-24 relative) of a value whose logits and
+# 64-bit logarithm of a sum of float32 powers are good to 2^-22 absolute
+LOGP_ABS, LOGP_REL = 2.0 ** -22, 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def sampler():
+    ensure_built()
+    s = as2d.Sampler(64, 31, 160000)
+    yield s
+    s.close()
+
+
+def heap(k, branch):
+    return [i // branch - 1 for i in range(k)]
+
+
+def inputs(n, k, vocab, branch, dtype=torch.float32, pad=0, seed=0, spread=2.0, temperature=1.0, noise=0.7):
+    g = torch.Generator().manual_seed(seed)
+    t = spread * torch.randn((n, k + 1, vocab), generator=g)
+    d = t + noise * torch.randn((n, k + 1, vocab), generator=g)
+    t, d = t.to(dtype), d.to(dtype)
+    cands = torch.zeros((n, k), dtype=torch.int32)
+    for i, p in enumerate(heap(k, branch)):
+        cands[:, i] = torch.multinomial(torch.softmax(d[:, p + 1].double() / temperature, -1), 1, generator=g)[:, 0].int()
+    u = torch.rand((n, k + 1), generator=g)
+
+    def rows(x):
+        out = torch.full((n, k + 1, vocab + pad), float("nan"), dtype=dtype, device="cuda")[:, :, :vocab]
+        return out.copy_(x)
+    return rows(t), rows(d), cands.cuda(), u.cuda()
+
+
+def check(got, target, cands, u, parents, draft=None, temperature=1.0, draft_temperature=None, ks=None):
+    got = {name: x.cpu() for name, x in got.items()}
+    n, rows, vocab = target.shape
+    k = rows - 1
+    t = target.double().cpu().numpy()
+    d = None if draft is None else draft.double().cpu().numpy()
+    for r in range(n):
+        kr = k if ks is None else ks[r]
+        temp = float(temperature[r]) if hasattr(temperature, "__len__") else temperature
+        uu = u[r].cpu().numpy()
+        path, token, logp = trees.sample_walk(t[r, :kr + 1], cands[r, :kr].cpu().numpy(), np.append(uu[:kr], uu[k]), parents[:kr],
+                                              temp, None if d is None else d[r], draft_temperature)
+        assert got["path"][r].tolist() == path + [-1] * (k - len(path)), r
+        assert (int(got["accepted"][r]), int(got["token"][r])) == (len(path), token), r
+        mine = np.append(got["logp"][r, :kr].numpy(), got["logp"][r, k].numpy())
+        # float32's range ends at 3.4e38: a finite -6e38 of 64 bits is its -inf
+        with np.errstate(over="ignore"):
+            fine = np.isfinite(np.asarray(logp).astype(np.float32))
+        assert np.array_equal(np.isfinite(mine), fine)
+        assert (np.abs(mine[fine] - np.array(logp)[fine]) <= LOGP_ABS + LOGP_REL * np.abs(np.array(logp)[fine])).all(), r
+        assert torch.isnan(got["logp"][r, kr:k]).all()
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+@pytest.mark.parametrize("n,k,vocab,branch", [(1, 0, 1, 1), (1, 0, 5, 1), (3, 1, 2, 1), (2, 4, 17, 1), (64, 3, 100, 2),
+                                              (1, 31, 4096, 1), (2, 31, 4097, 31), (5, 8, 8191, 3), (1, 8, 152064, 1),
+                                              (3, 15, 50257, 4)])
+def test_against_the_oracle(sampler, n, k, vocab, branch, with_draft):
+    t, d, cands, u = inputs(n, k, vocab, branch, seed=n + k + vocab)
+    d = d if with_draft else None
+    check(sampler.verify(t, cands, u, parents=heap(k, branch), draft_logits=d), t, cands, u, heap(k, branch), d)
+
+
+@pytest.mark.parametrize("pad", [0, 1, 3, 8])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_types_and_strides(sampler, dtype, pad):
+    """Rows at any element's address; what lies between them (NaN here) is not read."""
+    t, d, cands, u = inputs(3, 5, 5001, 2, dtype, pad, seed=pad, temperature=0.6)
+    got = sampler.verify(t, cands, u, parents=heap(5, 2), draft_logits=d, temperature=0.6)
+    check(got, t, cands, u, heap(5, 2), d, 0.6)
+
+
+def test_temperatures(sampler):
+    t, d, cands, u = inputs(4, 4, 3000, 1, seed=9)
+    temps = torch.tensor([0.05, 0.5, 1.0, 4.0], device="cuda")
+    check(sampler.verify(t, cands, u, draft_logits=d, temperature=temps, draft_temperature=1.3), t, cands, u, trees.chain(4), d,
+          temps.cpu(), 1.3)
+    check(sampler.verify(t, cands, u, draft_logits=d, temperature=temps), t, cands, u, trees.chain(4), d, temps.cpu())
+
+
+def test_ragged_requests(sampler):
+    """ks[r] candidates of k; logits, candidates and numbers past them are garbage."""
+    t, d, cands, u = inputs(4, 6, 700, 2, seed=4)
+    ks = [0, 1, 4, 6]
+    for r, kr in enumerate(ks):
+        t[r, kr + 1:] = float("nan")
+        d[r, kr + 1:] = float("inf")
+        cands[r, kr:] = -77
+        u[r, kr:6] = float("nan")
+    dev = torch.tensor(ks, dtype=torch.int32, device="cuda")
+    for draft in (None, d):
+        check(sampler.verify(t, cands, u, parents=heap(6, 2), ks=dev, draft_logits=draft), t, cands, u, heap(6, 2), draft, ks=ks)
+
+
+def test_a_drafter_s_rows_without_children_are_not_read(sampler):
+    t, d, cands, u = inputs(2, 4, 900, 2, seed=5)
+    d[:, 2:] = float("nan")   # rows 0 and 1 have the four children
+    got = sampler.verify(t, cands, u, parents=[-1, -1, 0, 0], draft_logits=d)
+    check(got, t, cands, u, [-1, -1, 0, 0], d)
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_masked_tokens(sampler, with_draft):
+    """-inf logits are tokens of probability 0, whole chunks of them too; one allowed token is certain."""
+    t, d, cands, u = inputs(3, 3, 9000, 1, seed=6)
+    t[:, :, 100:8500] = -float("inf")
+    t[1, 0] = -float("inf")
+    t[1, 0, 4242] = -3.0
+    t[2, 1, :] = -3.0e38
+    t[2, 1, 17] = 3.0e38
+    d = d if with_draft else None
+    got = sampler.verify(t, cands, u, draft_logits=d)
+    check(got, t, cands, u, trees.chain(3), d)
+
+
+def test_the_same_candidate_twice(sampler):
+    """A rejected token has no probability left when a sibling repeats it."""
+    t, _, cands, u = inputs(1, 4, 50, 4, seed=7)
+    cands[0] = torch.tensor([3, 3, 8, 3], dtype=torch.int32)
+    u[0, :4] = 0.999999
+    u[0, 4] = 0.0
+    check(sampler.verify(t, cands, u, parents=[-1] * 4), t, cands, u, [-1] * 4)
+
+
+def test_candidates_outside_the_vocabulary_are_never_accepted(sampler):
+    t, d, cands, u = inputs(1, 3, 60, 1, seed=8)
+    cands[0] = torch.tensor([-1, 60, 2 ** 31 - 1], dtype=torch.int32)
+    u[0, :3] = 0.0
+    for draft in (None, d):
+        got = sampler.verify(t, cands, u, parents=[-1, -1, -1], draft_logits=draft)
+        assert int(got["accepted"][0]) == 0 and 0 <= int(got["token"][0]) < 60
+        assert torch.isinf(got["logp"][0, :3]).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("where", ["target", "draft"])
+def test_non_finite_logits_end_their_request_only(sampler, where, value):
+    t, d, cands, u = inputs(3, 3, 5000, 1, seed=10)
+    (t if where == "target" else d)[1, 2, 4999] = value
+    got = sampler.verify(t, cands, u, draft_logits=d)
+    assert got["accepted"].tolist()[1] == got["token"].tolist()[1] == -1
+    assert got["path"][1].tolist() == [-1] * 3 and torch.isnan(got["logp"][1]).all()
+    keep = [0, 2]
+    check({name: x[keep] for name, x in got.items()}, t[keep], cands[keep], u[keep], trees.chain(3), d[keep])
+
+
+def test_rows_of_minus_infinity_and_bad_parameters(sampler):
+    t, d, cands, u = inputs(5, 2, 300, 1, seed=11)
+    t[0, 1] = -float("inf")
+    ks = torch.tensor([2, 3, -1, 2, 2], dtype=torch.int32, device="cuda")
+    temps = torch.tensor([1.0, 1.0, 1.0, 0.0, float("nan")], device="cuda")
+    got = sampler.verify(t, cands, u, ks=ks, temperature=temps)
+    assert got["accepted"].tolist() == [-1] * 5 and got["token"].tolist() == [-1] * 5
+    assert torch.isnan(got["logp"]).all()
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_random_numbers_next_to_a_border(sampler, with_draft):
+    """The float32 numbers on either side of the acceptance border p(x) / q(x), and the last and first of the range."""
+    t, d, cands, _ = inputs(1, 1, 2000, 1, seed=12, noise=1.5)
+    x = int(cands[0, 0])
+    p = np.exp(trees.log_softmax(t[0, 0].double().cpu().numpy(), 1.0))[x]
+    q = np.exp(trees.log_softmax(d[0, 0].double().cpu().numpy(), 1.0))[x] if with_draft else 1.0
+    border = np.float32(min(p / q, 0.9))
+    us = [0.0, 1 - 2.0 ** -24, border]
+    for step in range(2, 5):   # float32 powers leave 2^-23 of the border open
+        lo = hi = border
+        for _ in range(4 * step):
+            lo, hi = np.nextafter(lo, np.float32(0)), np.nextafter(hi, np.float32(1))
+        us += [lo, hi]
+    us = [w for w in us if w != border]
+    n = len(us)
+    u = torch.tensor([[w, 0.3] for w in us], dtype=torch.float32, device="cuda")
+    tt, dd, cc = t.expand(n, -1, -1).contiguous(), d.expand(n, -1, -1).contiguous(), cands.expand(n, -1).contiguous()
+    dd = dd if with_draft else None
+    check(sampler.verify(tt, cc, u, draft_logits=dd), tt, cc, u, [-1], dd)
+
+
+def test_the_extremes_of_the_last_number(sampler):
+    t, d, cands, u = inputs(2, 2, 6000, 1, seed=13)
+    u[0, 2], u[1, 2] = 0.0, 1 - 2.0 ** -24
+    for draft in (None, d):
+        check(sampler.verify(t, cands, u, draft_logits=draft), t, cands, u, trees.chain(2), draft)
+
+
+def test_committed_tokens_follow_the_target(sampler):
+    """64 x 400 calls: the first committed token's frequencies within five standard deviations of the target's."""
+    V, k, branch = 7, 4, 2
+    g = torch.Generator().manual_seed(14)
+    t1, d1 = 1.5 * torch.randn((k + 1, V), generator=g), 1.5 * torch.randn((k + 1, V), generator=g)
+    p = torch.softmax(t1[0].double(), -1).numpy()
+    count, n = np.zeros(V), 64 * 400
+    t, d = t1.expand(64, -1, -1).contiguous().cuda(), d1.expand(64, -1, -1).contiguous().cuda()
+    for _ in range(400):
+        cands = torch.stack([torch.multinomial(torch.softmax(d1[q + 1], -1), 64, replacement=True, generator=g)
+                             for q in heap(k, branch)], 1).int().cuda()
+        got = sampler.verify(t, cands, torch.rand((64, k + 1), generator=g).cuda(), parents=heap(k, branch), draft_logits=d)
+        path, token, c = got["path"].cpu(), got["token"].cpu(), cands.cpu()
+        first = torch.where(path[:, 0] >= 0, c.gather(1, path[:, :1].clamp(min=0).long())[:, 0], token)
+        count += np.bincount(first.numpy(), minlength=V)
+    assert (np.abs(count / n - p) <= 5 * np.sqrt(p * (1 - p) / n)).all()
+
+
+def test_a_replayed_graph_and_other_streams(sampler):
+    """Captured once, replayed with new inputs and other calls of the sampler in between."""
+    t, d, cands, u = inputs(2, 6, 20000, 2, seed=15)
+    other = inputs(3, 3, 9000, 1, seed=16)
+    sampler.verify(t, cands, u, parents=heap(6, 2), draft_logits=d)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = sampler.verify(t, cands, u, parents=heap(6, 2), draft_logits=d)
+    for seed in (17, 18, 19):
+        nt, nd, nc, nu = inputs(2, 6, 20000, 2, seed=seed)
+        for a, b in ((t, nt), (d, nd), (cands, nc), (u, nu)):
+            a.copy_(b)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(got, t, cands, u, heap(6, 2), d)
+        with torch.cuda.stream(side):
+            check(sampler.verify(other[0], other[2], other[3]), other[0], other[2], other[3], trees.chain(3))
+        check(sampler.verify(other[0], other[2], other[3], draft_logits=other[1]), other[0], other[2], other[3], trees.chain(3),
+              other[1])
+        torch.cuda.synchronize()
+
+
+def test_two_streams_in_turn(sampler):
+    """Calls on two streams with nothing waited for in between share the workspace in order."""
+    a, b = inputs(4, 8, 60000, 1, seed=20), inputs(4, 8, 60000, 2, seed=21)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        with torch.cuda.stream(s1):
+            got.append((sampler.verify(a[0], a[2], a[3], draft_logits=a[1]), a, 1))
+        with torch.cuda.stream(s2):
+            got.append((sampler.verify(b[0], b[2], b[3], parents=heap(8, 2), draft_logits=b[1]), b, 2))
+    torch.cuda.synchronize()
+    for out, x, branch in got:
+        check(out, x[0], x[2], x[3], heap(8, branch), x[1])
+
+
+def test_refusals(sampler):
+    t, d, cands, u = inputs(2, 3, 100, 1, seed=22)
+
+    def refused(**kw):
+        args = dict(logits=t, cands=cands, uniforms=u)
+        args.update(kw)
+        with pytest.raises(as2d.As2dError) as e:
+            sampler.verify(**args)
+        assert e.value.code == as2d.EINVAL, e.value
+    refused(parents=[-1, 1, 0])
+    refused(parents=[-2, 0, 1])
+    refused(parents=[-1, 0])
+    refused(temperature=0.0)
+    refused(temperature=float("nan"))
+    refused(temperature=float("inf"))
+    refused(draft_logits=d, draft_temperature=-1.0)
+    refused(cands=cands.long())
+    refused(cands=cands[:, :2])
+    refused(cands=cands.cpu())
+    refused(uniforms=u.double())
+    refused(uniforms=u[:1])
+    refused(logits=t.half())
+    refused(logits=t[0])
+    refused(logits=t.transpose(1, 2).contiguous().transpose(1, 2))
+    refused(draft_logits=d.bfloat16())
+    refused(draft_logits=d[:1])
+    refused(ks=torch.tensor([3], dtype=torch.int32, device="cuda"))
+    refused(temperature=torch.ones(3, device="cuda"))
+    small = as2d.Sampler(1, 2, 50)
+    for kw in (dict(), dict(logits=t[:1], cands=cands[:1], uniforms=u[:1])):
+        with pytest.raises(as2d.As2dError):
+            small.verify(**dict(dict(logits=t, cands=cands, uniforms=u), **kw))
+    small.close()
+
+
+def test_no_requests(sampler):
+    got = sampler.verify(torch.empty((0, 4, 10), device="cuda"), torch.empty((0, 3), dtype=torch.int32, device="cuda"),
+                         torch.empty((0, 4), device="cuda"))
+    assert got["accepted"].shape == (0,) and got["path"].shape == (0, 3)
