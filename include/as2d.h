@@ -194,14 +194,14 @@ int as2d_verify_static(as2d_ctx* ctx, int32_t req, const int32_t* cands, int32_t
  *
  * Errors, per-request non-finite logits and limits as in as2d_verify_batch
  * (AS2D_EINVAL also for a parent that does not come before its child, a
- * temperature that is not positive and finite, a random number outside [0, 1)).
+ * temperature outside [1e-30, 1e30], a random number outside [0, 1)).
  * Passes over trees run as AS2D_EXEC_GRAPH where the mode is
  * AS2D_EXEC_PERSISTENT.  A sampling call allocates device memory at its first
  * use and when a call needs more (the drafter's logits it copies, and a
  * workspace of about 40 bytes per row and 4,096 tokens).
  */
 typedef struct {
-  double temperature;        /* > 0: p = softmax(logits / temperature) */
+  double temperature;        /* 1e-30 to 1e30: p = softmax(logits / temperature) */
   double draft_temperature;  /* of the drafter's logits; 0: temperature */
   const float* uniforms;     /* host, k + 1 numbers in [0, 1): [i] tests candidate i, [k] draws the token after the path */
   const float* draft_logits; /* host or device, or NULL (candidates that come with no distribution): [.][vocab], row r the
@@ -269,8 +269,8 @@ int as2d_write_kv(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t pos, int32_
  *
  * A logit of -inf is a token of probability 0.  A request with a NaN or +inf
  * in a row (rows without children of draft_logits and rows past ks[r] are not
- * read), a row of -inf alone, ks[r] outside [0, k] or a temperature that is not
- * positive and finite gets accepted = token = -1, its path -1 and its logp NaN.
+ * read), a row of -inf alone, ks[r] outside [0, k] or a temperature outside
+ * [1e-30, 1e30] gets accepted = token = -1, its path -1 and its logp NaN.
  * A candidate outside [0, vocab) is never accepted.
  *
  * as2d_sampler_create allocates the workspace of calls of up to max_requests

@@ -176,21 +176,28 @@ def _ptr(a: np.ndarray) -> int:
     return a.ctypes.data
 
 
-_TYPES = {"torch.float32": F32, "torch.bfloat16": BF16}
-
-
 def _refuse(what: str):
     raise As2dError(EINVAL, what)
 
 
+_dtypes = {}
+
+
+def _types() -> dict:
+    """The library's type of each torch type it takes."""
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.float32: F32, torch.bfloat16: BF16})
+    return _dtypes
+
+
 def _on_device(t, name: str, dtype, shape) -> int:
-    """Checks a device tensor (torch) and returns its address; a None in
-    `shape` stands for any size."""
+    """Checks a device tensor (torch) and returns its address."""
     if not getattr(t, "is_cuda", False):
         _refuse(f"{name}: a device tensor is wanted")
-    if dtype is not None and str(t.dtype) != dtype:
+    if t.dtype != dtype:
         _refuse(f"{name}: {dtype} is wanted, not {t.dtype}")
-    if len(t.shape) != len(shape) or any(w is not None and w != s for w, s in zip(shape, t.shape)):
+    if t.shape != shape:
         _refuse(f"{name}: shape {tuple(shape)} is wanted, not {tuple(t.shape)}")
     return t.data_ptr()
 
@@ -203,36 +210,39 @@ def _dense(t, name: str, dtype, shape) -> int:
 
 
 def _rows(t, name: str, dtype, shape) -> Rows:
-    p = _on_device(t, name, dtype, shape)
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    p, stride = _on_device(t, name, dtype, shape), t.stride()
+    if stride[2] != 1 and shape[2] > 1:
         _refuse(f"{name}: adjacent dimensions are wanted")
-    return Rows(p, t.stride(0), t.stride(1))
+    return Rows(p, stride[0], stride[1])
 
 
-def _same_device(tensors):
-    if len({t.device for t in tensors}) > 1:
-        _refuse("tensors on several devices")
+def _one_device(tensors) -> int:
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != dev:
+            _refuse("tensors on several devices")
+    return dev
 
 
-def _stream_of(t, stream: Optional[int]) -> int:
-    """The given stream's handle, or the current torch stream of the tensor's device."""
+def _stream_of(device: int, stream: Optional[int]) -> int:
+    """The given stream's handle, or torch's current stream of the device."""
     if stream is not None:
         return stream
     import torch
-    return torch.cuda.current_stream(t.device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _int32(values) -> np.ndarray:
     return np.ascontiguousarray(values, dtype=np.int32)
 
 
-def _parents(parents, k: int) -> Optional[np.ndarray]:
+def _parents(parents, k: int):
+    """A host array of k parents, or None (null: a chain)."""
     if parents is None:
         return None
-    p = _int32(parents)
-    if p.shape != (k,):
-        _refuse(f"parents: {k} entries are wanted, not {p.shape}")
-    return p
+    if len(parents) != k:
+        _refuse(f"parents: {k} entries are wanted, not {len(parents)}")
+    return (ctypes.c_int32 * max(k, 1))(*parents)
 
 
 def _opt(a: Optional[np.ndarray]):
@@ -353,8 +363,11 @@ class Model:
         flat = _int32(np.concatenate(cands)) if n else _int32([])
         up = None
         if parents is not None:
-            up = _int32(np.concatenate([_int32(range(-1, len(c) - 1)) if p is None else _parents(p, len(c))
-                                        for p, c in zip(parents, cands)])) if n else None
+            for p, c in zip(parents, cands):
+                if p is not None and len(p) != len(c):
+                    _refuse(f"parents: {len(c)} entries are wanted, not {len(p)}")
+            up = _int32(np.concatenate([_int32(range(-1, len(c) - 1) if p is None else p) for p, c in zip(parents, cands)])) \
+                if n else None
         paths = np.full(max(flat.size, 1), -1, np.int32)
         outs, args, keep = (VerifyOut * max(n, 1))(), None, []
         if sampling is not None:
@@ -383,14 +396,11 @@ class Model:
                 d = np.ascontiguousarray(d, dtype=np.float32)
                 p = _ptr(d)
             else:
-                p = _dense(d, "draft_logits", "torch.float32", (None, self.shape.vocab))
                 import torch
+                p = _dense(d, "draft_logits", torch.float32, tuple(d.shape))
                 torch.cuda.current_stream(d.device).synchronize()   # the pass copies from it on its own stream
             keep.append(d)
         return Sampling(s.get("temperature", 1.0), s.get("draft_temperature", 0.0), _ptr(u), p)
-
-    def _model_type(self) -> str:
-        return "torch.float32" if self.shape.dtype == F32 else "torch.bfloat16"
 
     def tree_attention(self, req: int, layer: int, q, k, v, parents: Optional[Sequence[int]] = None, out=None,
                        stream: Optional[int] = None):
@@ -398,30 +408,29 @@ class Model:
         (as2d_tree_attention): q [rows, n_q_heads, head_dim], k and v
         [rows, n_kv_heads, head_dim], device tensors of the model's type, on
         the current torch stream or `stream`.  Returns out (new if None)."""
-        s, t, rows = self.shape, self._model_type(), q.shape[0]
-        a = [_rows(q, "q", t, (None, s.n_q_heads, s.head_dim)), _rows(k, "k", t, (rows, s.n_kv_heads, s.head_dim)),
-             _rows(v, "v", t, (rows, s.n_kv_heads, s.head_dim))]
+        s, rows, t = self.shape, q.shape[0], q.dtype
+        if _types().get(t) != s.dtype:
+            _refuse(f"tree_attention: {t} tensors, the model's type is {s.dtype}")
         if rows < 1:
             _refuse("tree_attention: no rows")
-        p = _parents(parents, rows - 1)
+        q_shape, kv_shape = (rows, s.n_q_heads, s.head_dim), (rows, s.n_kv_heads, s.head_dim)
         if out is None:
-            out = q.new_empty((rows, s.n_q_heads, s.head_dim))
-        a.append(_rows(out, "out", t, (rows, s.n_q_heads, s.head_dim)))
-        _same_device([q, k, v, out])
-        self._check(self.lib.as2d_tree_attention(self.ctx, req, layer, rows, _opt(p), *a, _stream_of(q, stream)))
+            out = q.new_empty(q_shape)
+        self._check(self.lib.as2d_tree_attention(
+            self.ctx, req, layer, rows, _parents(parents, rows - 1), _rows(q, "q", t, q_shape), _rows(k, "k", t, kv_shape),
+            _rows(v, "v", t, kv_shape), _rows(out, "out", t, q_shape), _stream_of(_one_device((q, k, v, out)), stream)))
         return out
 
     def write_kv(self, req: int, layer: int, k, v, pos: int = 0, stream: Optional[int] = None):
         """Keys and values [n, n_kv_heads, head_dim] (device, float32 or
         bfloat16) into positions pos .. of one layer of the request's cache."""
-        s = self.shape
-        if str(k.dtype) not in _TYPES:
-            _refuse(f"k: float32 or bfloat16 is wanted, not {k.dtype}")
-        a = [_rows(t, name, str(k.dtype), (k.shape[0], s.n_kv_heads, s.head_dim)) for t, name in ((k, "k"), (v, "v"))]
-        _same_device([k, v])
+        s, t = self.shape, k.dtype
+        if t not in _types():
+            _refuse(f"k: float32 or bfloat16 is wanted, not {t}")
+        a = [_rows(x, name, t, (k.shape[0], s.n_kv_heads, s.head_dim)) for x, name in ((k, "k"), (v, "v"))]
+        dev = _one_device((k, v))
         if k.shape[0]:
-            self._check(self.lib.as2d_write_kv(self.ctx, req, layer, pos, k.shape[0], _TYPES[str(k.dtype)], *a,
-                                               _stream_of(k, stream)))
+            self._check(self.lib.as2d_write_kv(self.ctx, req, layer, pos, k.shape[0], _types()[t], *a, _stream_of(dev, stream)))
 
     def verify_batch_status(self, reqs: Sequence[int], cands: Sequence[Sequence[int]]):
         """as2d_verify_batch returning (status, per-request results) without
@@ -577,50 +586,47 @@ class Sampler:
         token [n] and logp [n, k + 1], on the current torch stream or
         `stream`."""
         import torch
-        if len(getattr(logits, "shape", ())) != 3:
-            _refuse("logits: [n, k + 1, vocab] is wanted")
-        n, rows, vocab = logits.shape
+        shape, t = getattr(logits, "shape", ()), getattr(logits, "dtype", None)
+        if len(shape) != 3 or shape[1] < 1 or t not in _types():
+            _refuse("logits: [n, k + 1, vocab], float32 or bfloat16, is wanted")
+        n, rows, vocab = shape
         k = rows - 1
-        if str(logits.dtype) not in _TYPES or k < 0:
-            _refuse("logits: float32 or bfloat16 and at least one row a request are wanted")
-        a = SampleArgs()
-        a.n, a.k, a.vocab, a.dtype = n, k, vocab, _TYPES[str(logits.dtype)]
-        p = _parents(parents, k)
-        a.parents = _opt(p)
         tensors = [logits, uniforms]
-        a.logits, a.row_stride = self._logits(logits, "logits", logits)
-        a.uniforms = _dense(uniforms, "uniforms", "torch.float32", (n, rows))
+        p_logits, step = self._logits(logits, "logits", t, shape)
+        p_draft, p_cands, p_ks, p_temps, draft_step = None, None, None, None, 0
         if k:
-            a.cands = _dense(cands, "cands", "torch.int32", (n, k))
+            p_cands = _dense(cands, "cands", torch.int32, (n, k))
             tensors.append(cands)
         if draft_logits is not None:
-            a.draft_logits, a.draft_row_stride = self._logits(draft_logits, "draft_logits", logits)
+            p_draft, draft_step = self._logits(draft_logits, "draft_logits", t, shape)
             tensors.append(draft_logits)
         if ks is not None:
-            a.ks = _dense(ks, "ks", "torch.int32", (n,))
+            p_ks = _dense(ks, "ks", torch.int32, (n,))
             tensors.append(ks)
         if hasattr(temperature, "data_ptr"):
-            a.temperatures = _dense(temperature, "temperature", "torch.float32", (n,))
+            p_temps = _dense(temperature, "temperature", torch.float32, (n,))
             tensors.append(temperature)
-        else:
-            a.temperature = temperature
-        a.draft_temperature = draft_temperature
-        _same_device(tensors)
-        i32 = uniforms.new_empty((n * (k + 2),), dtype=torch.int32)
-        out = dict(accepted=i32[:n], token=i32[n:2 * n], path=i32[2 * n:].view(n, k), logp=uniforms.new_empty((n, rows)))
-        a.accepted, a.token, a.path, a.logp = (out[x].data_ptr() for x in ("accepted", "token", "path", "logp"))
-        rc = self.lib.as2d_sampler_verify(self.h, ctypes.byref(a), _stream_of(logits, stream))
+            temperature = 0.0
+        p_uniforms = _dense(uniforms, "uniforms", torch.float32, (n, rows))
+        dev = _one_device(tensors)
+        new = cands if k else uniforms.new_empty(0, dtype=torch.int32)
+        out = dict(accepted=new.new_empty(n), path=new.new_empty((n, k)), token=new.new_empty(n),
+                   logp=uniforms.new_empty((n, rows)))
+        up = _parents(parents, k)
+        a = SampleArgs(n, k, vocab, _types()[t], p_logits, step, p_draft, draft_step, p_cands,
+                       ctypes.addressof(up) if up is not None and k else None, p_ks, p_uniforms, p_temps, temperature,
+                       draft_temperature, *(x.data_ptr() for x in out.values()))
+        rc = self.lib.as2d_sampler_verify(self.h, a, _stream_of(dev, stream))
         if rc != OK:
             raise As2dError(rc, self.lib.as2d_sampler_last_error(self.h).decode())
         return out
 
     @staticmethod
-    def _logits(t, name, like):
+    def _logits(t, name, dtype, shape):
         """(address, elements between rows) of [n, rows, vocab] logits whose rows are evenly apart."""
-        p = _on_device(t, name, str(like.dtype), tuple(like.shape))
-        n, rows, vocab = t.shape
-        step = t.stride(1) if rows > 1 else t.stride(0) if n > 1 else vocab
-        if (vocab > 1 and t.stride(2) != 1) or (n > 1 and rows > 1 and t.stride(0) != rows * step):
+        p, (n, rows, vocab), stride = _on_device(t, name, dtype, shape), shape, t.stride()
+        step = stride[1] if rows > 1 else stride[0] if n > 1 else vocab
+        if (vocab > 1 and stride[2] != 1) or (n > 1 and rows > 1 and stride[0] != rows * step):
             _refuse(f"{name}: rows of adjacent logits, evenly apart, are wanted")
         return p, step
 

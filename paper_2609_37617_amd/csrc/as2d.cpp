@@ -1038,8 +1038,9 @@ int assemble_tree(as2d_ctx* c, int n, const int32_t* parents, const int32_t* ks,
     *max_children = std::max(*max_children, children);
     if (!sampling) continue;
     const as2d_sampling& s = sampling[r];
-    if (!(s.temperature > 0.0) || !std::isfinite(s.temperature) || s.draft_temperature < 0.0 || !std::isfinite(s.draft_temperature))
-      return fail(c, AS2D_EINVAL, "verify: temperature %g, %g of request %d (> 0, and >= 0)", s.temperature, s.draft_temperature, r);
+    const auto good = [](double t) { return t >= kLeastTemp && t <= kMostTemp; };
+    if (!good(s.temperature) || (s.draft_temperature != 0.0 && !good(s.draft_temperature)))
+      return fail(c, AS2D_EINVAL, "verify: temperature %g, of the drafter %g (1e-30 to 1e30)", s.temperature, s.draft_temperature);
     if (!s.uniforms) return fail(c, AS2D_EINVAL, "verify: null random numbers");
     for (int i = 0; i <= k; ++i) {
       if (!(s.uniforms[i] >= 0.f && s.uniforms[i] < 1.f))
@@ -1100,9 +1101,13 @@ int launch_sampling(as2d_ctx* c, int n, int max_k, int max_children, bool draft)
   a.chunks = (a.vocab + kSampleChunk - 1) / kSampleChunk;
   a.n = n;
   a.k = max_k;
-  const int rc = grow(c, &c->sample_work, &c->sample_cap, sample_layout(a, max_children, nullptr));
+  a.max_children = max_children;
+  const int mr = c->cfg.max_requests;
+  const size_t before = c->sample_cap;
+  const int rc = grow(c, &c->sample_work, &c->sample_cap, sample_layout(a, mr, nullptr));
   if (rc) return rc;
-  sample_layout(a, max_children, (char*)c->sample_work);
+  sample_layout(a, mr, (char*)c->sample_work);
+  if (c->sample_cap != before) HIP_TRY(c, launch_fill_zero(a.ticket, mr, c->stream));
   a.target = c->b.logits;
   a.draft = draft ? c->draft : nullptr;
   a.t_stride = a.d_stride = c->cfg.vocab;
@@ -1110,7 +1115,7 @@ int launch_sampling(as2d_ctx* c, int n, int max_k, int max_children, bool draft)
   a.rows = c->b.d_rows;
   a.gate = c->tree.sel;
   a.tree = c->tree;
-  HIP_TRY(c, launch_sample(a, draft, max_children, c->stream));
+  HIP_TRY(c, launch_sample(a, draft, c->stream));
   return AS2D_OK;
 }
 

@@ -328,24 +328,18 @@ struct SampleReq {
   int32_t draft_row0;          // first row of the drafter's logits, -1: none
   int32_t pad;
 };
-struct SamplePart {            // one chunk of a row: maximum, sum of 2^((x - max) c), whether a value is NaN or +inf
-  double sum;
-  float max;
-  int bad;
-};
-struct SampleDecision {
-  int bad, accepted, node, n_gone;   // node: the row whose distribution gives the token
-  double u, cut;                     // its random number; multiples of the drafter's distribution taken off
-  double c, log_sum, dc, dlog_sum;   // log2(e) / temperature and log2 of the sum, target and drafter
-  float max, dmax;
-  int draft, pad;
-  int gone[32];                      // rejected candidates of the node (no drafter)
+// Temperatures: x / T stays far inside 64 bits' range for every float32 x.
+constexpr double kLeastTemp = 1e-30, kMostTemp = 1e30;
+
+struct SamplePart {            // one chunk of a row: sum of 2^(x c - top), top the least integer >= every x c (-inf: all
+  double sum, top;             // -inf; NaN: a value is NaN or +inf)
 };
 struct SampleArgs {
   const void* target;          // [rows][vocab], float32 or bf16
   const void* draft;           // the same of the drafter (row r: what row r's children were drawn from), or null
   long long t_stride, d_stride;
   int n, k, vocab, chunks;     // k: most candidates of a request; chunks of kSampleChunk logits
+  int max_children;            // most children of a row
   int bf16;
   // a pass of the verification step: requests and rows of its descriptors
   const SampleReq* reqs;
@@ -366,26 +360,27 @@ struct SampleArgs {
   double* stage;               // [max_children - 1][n][k + 1][chunks]
   double* cut;                 // [max_children][n][k + 1]
   double* left;                // [n][chunks]
-  SampleDecision* dec;         // [n]
+  int* ticket;                 // [n], zero between launches
 };
-constexpr int kSampleChunk = 4096;
-// Workspace of a (n, k, chunks set): its bytes; with base, points a's arrays into it.
-inline size_t sample_layout(SampleArgs& a, int max_children, char* base) {
+constexpr int kSampleChunk = 1024;
+// Workspace of a (n, k, chunks, max_children set): its bytes; with base, points a's
+// arrays into it.  The tickets come first, max_n of them: they are zeroed once.
+inline size_t sample_layout(SampleArgs& a, int max_n, char* base) {
   size_t off = 0;
   const auto take = [&](auto** p, size_t n) {
     *p = reinterpret_cast<std::remove_reference_t<decltype(**p)>*>(base + off);
     off += (n * sizeof(**p) + 255) / 256 * 256;
   };
-  const size_t rows = (size_t)a.n * (a.k + 1), stages = max_children > 1 ? max_children - 1 : 0;
+  const size_t rows = (size_t)a.n * (a.k + 1), stages = a.max_children > 1 ? a.max_children - 1 : 0;
+  take(&a.ticket, max_n);
   take(&a.part, 2 * rows * a.chunks);
   take(&a.stage, stages * rows * a.chunks);
   take(&a.cut, stages * rows);
   take(&a.left, (size_t)a.n * a.chunks);
-  take(&a.dec, a.n);
   return off;
 }
-// draft: some request has a drafter's logits; max_children: most children of a row.
-hipError_t launch_sample(const SampleArgs& a, bool draft, int max_children, hipStream_t s);
+// draft: some request has a drafter's logits.
+hipError_t launch_sample(const SampleArgs& a, bool draft, hipStream_t s);
 
 // Zeroes n ints (a kernel, not a memset, so that it may be captured).
 hipError_t launch_fill_zero(int* p, int n, hipStream_t s);

@@ -30,8 +30,8 @@ namespace as2d {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kPer = kSampleChunk / kThreads;   // logits of a thread
+constexpr int kPer = kSampleChunk / 64;   // logits of a lane
+constexpr int kBlock = 256, kWide = 1024;  // threads: one pass over the logits, and the kernels that also combine parts
 constexpr double kLog2E = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
 
 // ---- requests ---------------------------------------------------------------
@@ -60,7 +60,7 @@ __device__ __forceinline__ Req load_req(const SampleArgs& a, int r) {
     t = a.temps ? (double)a.temps[r] : a.temp;
     dt = a.draft_temp > 0.0 ? a.draft_temp : t;
   }
-  q.ok = q.k >= 0 && q.k <= a.k && t > 0.0 && t < INFINITY;
+  q.ok = q.k >= 0 && q.k <= a.k && t >= kLeastTemp && t <= kMostTemp;
   if (!q.ok) q.k = 0;
   q.c = kLog2E / t;
   q.dc = kLog2E / dt;
@@ -78,12 +78,13 @@ __device__ __forceinline__ int cand_of(const SampleArgs& a, const Req& q, int i)
 __device__ __forceinline__ float uniform_of(const SampleArgs& a, const Req& q, int i) {
   return a.reqs ? a.rows[q.row0 + i].u : a.uniforms[(size_t)q.r * (a.k + 1) + (i ? i - 1 : a.k)];
 }
-// Children of row `row`; every lane of the wave gets the count.
-__device__ __forceinline__ int children_of(const SampleArgs& a, const Req& q, int row) {
+// This lane's parent row (lane = row 1 .. k; -1 for the others), and the rows
+// that follow a row, as bits.
+__device__ __forceinline__ int lane_parent(const SampleArgs& a, const Req& q) {
   const int lane = threadIdx.x & 63;
-  const bool child = lane >= 1 && lane <= q.k && parent_of(a, q, lane) == row;
-  return __popcll(__ballot(child));
+  return lane >= 1 && lane <= q.k ? parent_of(a, q, lane) : -1;
 }
+__device__ __forceinline__ uint32_t children_of(int parent, int row) { return (uint32_t)__ballot(parent == row); }
 
 // ---- rows of logits ---------------------------------------------------------
 
@@ -92,13 +93,12 @@ template <bool BF> __device__ __forceinline__ float logit(const void* base, long
   else return ldg(static_cast<const float*>(base) + i);
 }
 
-// A thread's kPer logits of a chunk: runs of 16 bytes, kThreads apart (rows may
-// start at any element: the loads need no alignment past the element's).
-// Element e is column chunk * kSampleChunk + column<BF>(e); columns past the row
-// read -inf.
+// A lane's kPer logits of a wave's chunk: runs of 16 bytes, 64 lanes apart (rows
+// may start at any element: the loads need no alignment past the element's).
+// Columns past the row read -inf.
 template <bool BF> __device__ __forceinline__ int column(int e) {
   constexpr int RUN = BF ? 8 : 4;
-  return ((e / RUN) * kThreads + (int)threadIdx.x) * RUN + e % RUN;
+  return ((e / RUN) * 64 + (int)(threadIdx.x & 63)) * RUN + e % RUN;
 }
 template <bool BF> __device__ __forceinline__ void load_chunk(const void* base, long long row, int chunk, int vocab, float (&x)[kPer]) {
   constexpr int RUN = BF ? 8 : 4;
@@ -128,11 +128,10 @@ template <bool BF> __device__ __forceinline__ void load_chunk(const void* base, 
   }
 }
 
-// 2^((x - m) c) for x <= m.
-__device__ __forceinline__ float power(float x, float m, double c) {
-  const double y = ((double)x - (double)m) * c;
+// 2^(x c - top).
+__device__ __forceinline__ float power(float x, double c, double top) {
+  const double y = fmax(__builtin_fma((double)x, c, -top), -200.0);   // 2^-200 and less (x = -inf) are 0 in float32
   const float f = (float)y;
-  if (!(f > -160.f)) return 0.f;   // below float32's range; x = -inf
   return __builtin_amdgcn_exp2f(f) * __builtin_fmaf((float)(y - (double)f), (float)kLn2, 1.0f);
 }
 
@@ -146,24 +145,47 @@ __device__ __forceinline__ double left_of(float p, double ps, float q, double qs
 
 // ---- reductions: fixed trees, the same bits in every lane -------------------
 
+// (cross-lane moves that do not go through the LDS, a 32-bit half at a time)
+
+template <int CTRL, int ROWS = 0xF> __device__ __forceinline__ double dpp_get64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// op of lane l's and lane l ^ 16's (SWAP32: l ^ 32's) values, in the lower lane's order.
+template <bool SWAP32, class Op> __device__ __forceinline__ double swap64(double v, Op op) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t l = (uint32_t)u, h = (uint32_t)(u >> 32);
+  const auto swap = [](uint32_t w) {
+    if constexpr (SWAP32) return __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    else return __builtin_amdgcn_permlane16_swap(w, w, false, false);
+  };
+  const auto a = swap(l), b = swap(h);
+  return op(__builtin_bit_cast(double, (uint64_t)b[0] << 32 | a[0]), __builtin_bit_cast(double, (uint64_t)b[1] << 32 | a[1]));
+}
+template <class Op> __device__ __forceinline__ double wave_reduce64(double v, Op op) {
+  v = op(v, dpp_get64<kDppXor1>(v));
+  v = op(v, dpp_get64<kDppXor2>(v));
+  v = op(v, dpp_get64<kDppHalfMirror>(v));
+  v = op(v, dpp_get64<kDppMirror>(v));
+  return swap64<true>(swap64<false>(v, op), op);
+}
 __device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return wave_reduce64(v, [](double a, double b) { return a + b; });
+}
+__device__ __forceinline__ double wave_max64(double v) {
+  return wave_reduce64(v, [](double a, double b) { return fmax(a, b); });
+}
+// Running sums, this lane's included: within 16 lanes, then the rows before.
+__device__ __forceinline__ double wave_scan64(double v) {
+  v += dpp_get64<0x111>(v);        // row_shr 1, 2, 4, 8 (0 from before the row)
+  v += dpp_get64<0x112>(v);
+  v += dpp_get64<0x114>(v);
+  v += dpp_get64<0x118>(v);
+  v += dpp_get64<0x142, 0xA>(v);   // lane 15 of rows 0 and 2 to rows 1 and 3
+  v += dpp_get64<0x143, 0xC>(v);   // lane 31 to rows 2 and 3
   return v;
-}
-__device__ __forceinline__ double block_sum64(double v, double* s) {
-  v = wave_sum64(v);
-  __syncthreads();   // s may be in use
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (s[0] + s[1]) + (s[2] + s[3]);
-}
-__device__ __forceinline__ float block_max(float v, float* s) {
-  v = wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
 }
 
 // ---- workspace places ----------------------------------------------------------
@@ -178,44 +200,65 @@ __device__ __forceinline__ double* cut_of(const SampleArgs& a, int s, int r, int
   return a.cut + ((size_t)(s - 1) * a.n + r) * (a.k + 1) + row;
 }
 
-// A row's maximum, log2 of its sum and whether it has a value that is no
-// logit, from its chunks' parts; one wave, every lane gets them.
+// v 2^(from - to), both integers, from <= to.
+__device__ __forceinline__ double rescale(double v, double from, double to) { return ldexp(v, (int)fmax(from - to, -2000.0)); }
+
+// A row's sum of 2^(x c - top) from its chunks' parts (their tops are integers,
+// so nothing is rounded but the sum); bad: a value that is no logit, or none
+// that is finite.  One wave, every lane gets them.
 struct RowStat {
-  float max;
-  double log_sum;
-  bool bad;
+  double sum, top;
+  int bad;
 };
-__device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks, double c) {
+__device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks) {
   const int lane = threadIdx.x & 63;
-  float m = -INFINITY;
-  int bad = 0;
-  for (int i = lane; i < chunks; i += 64) {
-    m = fmaxf(m, part[i].max);
-    bad |= part[i].bad;
+  constexpr int B = 4;   // a lane's first parts, kept (262,144 tokens: all of them)
+  SamplePart p[B];
+  double top = -INFINITY;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < B; ++i) {
+    p[i] = SamplePart{0.0, -INFINITY};
+    if (64 * i + lane < chunks) p[i] = part[64 * i + lane];
   }
-  m = wave_max(m);
+#pragma unroll
+  for (int i = 0; i < B; ++i) {
+    bad |= p[i].top != p[i].top;
+    top = fmax(top, p[i].top);
+  }
+  for (int i = 64 * B + lane; i < chunks; i += 64) {
+    bad |= part[i].top != part[i].top;
+    top = fmax(top, part[i].top);
+  }
+  top = wave_max64(top);
   double s = 0.0;
-  for (int i = lane; i < chunks; i += 64)
-    if (part[i].max > -INFINITY) s += part[i].sum * exp2(((double)part[i].max - (double)m) * c);
-  s = wave_sum64(s);
-  return RowStat{m, log2(s), __ballot(bad) != 0 || !(m > -INFINITY)};
+#pragma unroll
+  for (int i = 0; i < B; ++i)
+    if (p[i].top > -INFINITY) s += rescale(p[i].sum, p[i].top, top);
+  for (int i = 64 * B + lane; i < chunks; i += 64)
+    if (part[i].top > -INFINITY) s += rescale(part[i].sum, part[i].top, top);
+  return RowStat{wave_sum64(s), top, __ballot(bad) != 0 || !(top > -INFINITY)};
 }
-__device__ __forceinline__ double prob(float x, float max, double c, double log_sum) {
-  return x > -INFINITY ? exp2(((double)x - (double)max) * c - log_sum) : 0.0;
+__device__ __forceinline__ double prob(float x, const RowStat& t, double c) {
+  return x > -INFINITY ? exp2(__builtin_fma((double)x, c, -t.top)) / t.sum : 0.0;
+}
+// log p of a token in natural units, rounded once.
+__device__ __forceinline__ float log_prob(float x, double top, double log_sum, double c) {
+  return x > -INFINITY ? (float)((__builtin_fma((double)x, c, -top) - log_sum) * kLn2) : -INFINITY;
 }
 
 // ---- kernels ----------------------------------------------------------------
 
 // Maximum and sum of every chunk of the target's rows and of the drafter's
-// rows with children.  The one pass over the logits that cannot be avoided.
+// rows with children, a chunk per wave.  The one pass over the logits that
+// cannot be avoided.
 template <bool BF>
-__global__ __launch_bounds__(kThreads) void sample_stats_kernel(const SampleArgs a) {
-  __shared__ float s_max[4];
-  __shared__ double s_sum[4];
-  const int chunk = blockIdx.x, row = blockIdx.y, which = (int)blockIdx.z >= a.n, r = blockIdx.z - which * a.n;
+__global__ __launch_bounds__(kBlock) void sample_stats_kernel(const SampleArgs a) {
+  const int chunk = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6), row = blockIdx.y;
+  const int which = (int)blockIdx.z >= a.n, r = blockIdx.z - which * a.n;
   const Req q = load_req(a, r);
-  if (!q.ok || row > q.k) return;
-  if (which && (q.drow0 < 0 || children_of(a, q, row) == 0)) return;
+  if (!q.ok || row > q.k || chunk >= a.chunks) return;
+  if (which && (q.drow0 < 0 || !children_of(lane_parent(a, q), row))) return;
   float x[kPer];
   load_chunk<BF>(which ? a.draft : a.target, (which ? q.drow0 + row : q.row0 + row) * (which ? a.d_stride : a.t_stride), chunk,
                  a.vocab, x);
@@ -227,361 +270,371 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(const SampleArgs
     bad |= !(x[e] < INFINITY);
     m = fmaxf(m, x[e]);
   }
-  m = block_max(m, s_max);
+  m = wave_max(m);
+  const double top = __ballot(bad) != 0 ? (double)NAN : m > -INFINITY ? ceil((double)m * c) : -INFINITY;
   double s = 0.0;
-  if (m > -INFINITY && m < INFINITY) {
+  if (top > -INFINITY) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) s += (double)power(x[e], m, c);
+    for (int e = 0; e < kPer; e += 4)
+      s += (double)((power(x[e], c, top) + power(x[e + 1], c, top)) + (power(x[e + 2], c, top) + power(x[e + 3], c, top)));
+    s = wave_sum64(s);
   }
-  s = block_sum64(s, s_sum);
-  const bool any = __syncthreads_or(bad);
-  if (threadIdx.x == 0) part_of(a, r, which, row)[chunk] = SamplePart{s, m, any};
+  if ((threadIdx.x & 63) == 0) part_of(a, r, which, row)[chunk] = SamplePart{s, top};
 }
 
-// Sum of max(p - C q, 0) over a chunk.
+// Sum of max(p - C q, 0) over a wave's chunk; ps, qs: 1 / sum and C / sum.
 template <bool BF>
-__device__ __forceinline__ double chunk_left(const SampleArgs& a, long long trow, long long drow, int chunk, float max,
-                                             double c, double log_sum, float dmax, double dc, double dlog_sum, double cut,
-                                             double* s_sum) {
+__device__ __forceinline__ double chunk_left(const SampleArgs& a, long long trow, long long drow, int chunk, double top,
+                                             double c, double ps, double dtop, double dc, double qs) {
   float x[kPer], y[kPer];
   load_chunk<BF>(a.target, trow, chunk, a.vocab, x);
   load_chunk<BF>(a.draft, drow, chunk, a.vocab, y);
-  const double ps = exp2(-log_sum), qs = cut * exp2(-dlog_sum);
   double s = 0.0;
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) s += left_of(power(x[e], max, c), ps, power(y[e], dmax, dc), qs);
-  return block_sum64(s, s_sum);
+  for (int e = 0; e < kPer; ++e) s += left_of(power(x[e], c, top), ps, power(y[e], dc, dtop), qs);
+  return wave_sum64(s);
 }
 
 // Stage s: the mass left at every node of more than s children after s
 // rejections.  Its C is the earlier C and the earlier mass.
 template <bool BF>
-__global__ __launch_bounds__(kThreads) void sample_stage_kernel(const SampleArgs a, const int s) {
-  __shared__ double s_sum[4];
-  const int chunk = blockIdx.x, row = blockIdx.y, r = blockIdx.z;
+__global__ __launch_bounds__(kWide) void sample_stage_kernel(const SampleArgs a, const int s) {
+  __shared__ RowStat s_stat[2];
+  __shared__ double s_cut;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int chunk = blockIdx.x * (kWide / 64) + wave, row = blockIdx.y, r = blockIdx.z;
   const Req q = load_req(a, r);
-  if (!q.ok || row > q.k || q.drow0 < 0 || children_of(a, q, row) <= s) return;
-  double cut = 1.0;
-  if (s > 1) {
-    const double* before = stage_of(a, s - 1, r, row);
-    double v = 0.0;
-    for (int i = threadIdx.x & 63; i < a.chunks; i += 64) v += before[i];
-    cut = *cut_of(a, s - 1, r, row) + wave_sum64(v);
+  if (!q.ok || row > q.k || q.drow0 < 0 || __popc(children_of(lane_parent(a, q), row)) <= s) return;
+  if (wave < 2) {
+    const RowStat t = row_stat(part_of(a, r, wave, row), a.chunks);
+    if (lane == 0) s_stat[wave] = t;
+  } else if (wave == 2) {
+    double cut = 1.0;
+    if (s > 1) {
+      const double* before = stage_of(a, s - 1, r, row);
+      double v = 0.0;
+      for (int i = lane; i < a.chunks; i += 64) v += before[i];
+      cut = *cut_of(a, s - 1, r, row) + wave_sum64(v);
+    }
+    if (lane == 0) {
+      s_cut = cut;
+      if (blockIdx.x == 0) *cut_of(a, s, r, row) = cut;
+    }
   }
-  const RowStat t = row_stat(part_of(a, r, 0, row), a.chunks, q.c), d = row_stat(part_of(a, r, 1, row), a.chunks, q.dc);
+  __syncthreads();
+  if (chunk >= a.chunks) return;
+  const RowStat t = s_stat[0], d = s_stat[1];
   const double left = t.bad || d.bad ? 0.0
-                                     : chunk_left<BF>(a, (q.row0 + row) * a.t_stride, (q.drow0 + row) * a.d_stride, chunk, t.max,
-                                                      q.c, t.log_sum, d.max, q.dc, d.log_sum, cut, s_sum);
-  if (threadIdx.x == 0) {
-    stage_of(a, s, r, row)[chunk] = left;
-    if (chunk == 0) *cut_of(a, s, r, row) = cut;
-  }
+                                     : chunk_left<BF>(a, (q.row0 + row) * a.t_stride, (q.drow0 + row) * a.d_stride, chunk, t.top,
+                                                      q.c, 1.0 / t.sum, d.top, q.dc, s_cut / d.sum);
+  if (lane == 0) stage_of(a, s, r, row)[chunk] = left;
 }
 
-// The walk: rows' statistics and the candidates' probabilities, all at once,
-// then the tests in order.  One workgroup per request.
-template <bool BF>
-__global__ __launch_bounds__(kThreads) void sample_decide_kernel(const SampleArgs a) {
-  __shared__ float s_max[2][32];
-  __shared__ double s_log[2][32], s_p[32], s_q[32], s_cut[32], s_mass[32];
-  __shared__ int s_parent[32], s_cand[32], s_bad;
-  const int r = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const Req q = load_req(a, r);
-  if (tid == 0) s_bad = !q.ok || (a.gate && a.gate[r].nan_flag);
+// A running sum over the workgroup: the first index with v > 0 whose sum up
+// to and with it passes `goal`, or the last with v > 0 (the goal is the whole
+// sum, up to rounding), or -1; *before receives the sum before it.  One value
+// per thread, in order.
+struct Find {
+  double wave[kWide / 64], before;
+  int first, last;
+};
+template <class Goal> __device__ __forceinline__ int find_in_run(double v, Goal&& goal_of, Find& f, double* before) {
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const double run = wave_scan64(v);
+  __syncthreads();   // f may be in use
+  if (tid == 0) {
+    f.first = 0x7fffffff;
+    f.last = -1;
+  }
+  if ((tid & 63) == 63) f.wave[wave] = run;
   __syncthreads();
-  for (int w = wave; w < 2 * (q.k + 1); w += 4) {
-    const int which = w & 1, row = w >> 1;
-    if (which && (q.drow0 < 0 || children_of(a, q, row) == 0)) continue;
-    if (!q.ok) continue;
-    const RowStat st = row_stat(part_of(a, r, which, row), a.chunks, which ? q.dc : q.c);
+  double base = 0.0, total = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWide / 64; ++w) {
+    if (w == wave) base = total;
+    total += f.wave[w];
+  }
+  const double goal = goal_of(total);
+  const bool some = v > 0.0, hit = some && base + run > goal;
+  const uint64_t hits = __ballot(hit), any = __ballot(some);
+  if ((tid & 63) == 0) {
+    if (hits) atomicMin(&f.first, (wave << 6) + __ffsll((unsigned long long)hits) - 1);
+    if (any) atomicMax(&f.last, (wave << 6) + 63 - __clzll((long long)any));
+  }
+  __syncthreads();
+  const int at = f.first != 0x7fffffff ? f.first : f.last;
+  if (tid == at) f.before = base + run - v;
+  __syncthreads();
+  if (before) *before = goal - f.before;
+  return at;
+}
+
+// The walk and the token.  Every test's outcome follows from its node's
+// earlier siblings having failed, so all are made at once, a candidate per
+// lane, and the walk follows bits.  `gridDim.x` workgroups per request: more
+// than one where a drafter's distribution may have to be taken off the
+// node's; each then makes the same walk, sums its share of what is left, and
+// the last to finish draws the token.
+template <bool BF>
+__global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a) {
+  constexpr int kWavesW = kWide / 64;
+  __shared__ RowStat s_stat[2][32];
+  __shared__ double s_left[32], s_again[32], s_log[32];
+  __shared__ uint32_t s_children[32];
+  __shared__ int s_cand[32], s_bad, s_at, s_n, s_path[32], s_last;
+  __shared__ double s_cut, s_cutoff[32];
+  __shared__ Find s_find;
+  const int r = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const bool writes = blockIdx.x == 0;
+  const Req q = load_req(a, r);
+  const bool drafted = q.drow0 >= 0;
+  if (tid == 0) s_bad = !q.ok || (a.gate && a.gate[r].nan_flag);
+  const int parent = lane_parent(a, q);
+  // candidates: what they need from memory, in flight while the rows' parts are combined
+  const bool cand = wave < 2 && lane >= 1 && lane <= q.k;   // wave 0: the tests, wave 1: log-probabilities
+  const float u_tok = uniform_of(a, q, 0);
+  int x = -1;
+  float u = 0.f, l = -INFINITY, dl = -INFINITY;
+  if (cand) {
+    x = cand_of(a, q, lane);
+    u = uniform_of(a, q, lane);
+    if (x >= 0 && x < a.vocab) {
+      l = logit<BF>(a.target, (q.row0 + parent) * a.t_stride + x);
+      if (drafted) dl = logit<BF>(a.draft, (q.drow0 + parent) * a.d_stride + x);
+    }
+  }
+  __syncthreads();
+  for (int w = wave; w < 2 * (q.k + 1) && q.ok; w += kWavesW) {
+    const int which = w > q.k, row = w - which * (q.k + 1);
+    const uint32_t children = children_of(parent, row);
+    if (!which && lane == 0) s_children[row] = children;
+    if (which && (!drafted || !children)) continue;
+    const RowStat st = row_stat(part_of(a, r, which, row), a.chunks);
     if (lane == 0) {
-      s_max[which][row] = st.max;
-      s_log[which][row] = st.log_sum;
+      s_stat[which][row] = st;
       if (st.bad) s_bad = 1;
     }
   }
-  // for candidate row i, the m-th child of its node (m >= 1): C and the mass after m
-  // rejections (the last child's mass is never used)
-  if (q.drow0 >= 0)
-    for (int i = 1 + wave; i <= q.k; i += 4) {
-      const int p = parent_of(a, q, i);
-      const bool before = lane >= 1 && lane <= i && parent_of(a, q, lane) == p;
-      const int m = __popcll(__ballot(before));
-      const bool more = m < children_of(a, q, p);
-      double v = 0.0, cut = 0.0;
-      if (more) {
+  // candidate i of a drafter's row: C and the mass once its m earlier siblings have been rejected
+  if (drafted && a.max_children > 1)
+    for (int i = 1 + wave; i <= q.k; i += kWavesW) {
+      const int p = __shfl(parent, i);
+      const int m = __popc(children_of(parent, p) & ((1u << i) - 1));
+      double v = m ? 0.0 : 1.0;
+      if (m) {
         for (int j = lane; j < a.chunks; j += 64) v += stage_of(a, m, r, p)[j];
-        cut = *cut_of(a, m, r, p);
-      } else if (m > 1) {
-        for (int j = lane; j < a.chunks; j += 64) v += stage_of(a, m - 1, r, p)[j];
-        cut = *cut_of(a, m - 1, r, p);
+        v = wave_sum64(v);
       }
-      v = wave_sum64(v);
       if (lane == 0) {
-        s_mass[i] = more ? v : 0.0;
-        s_cut[i] = more ? cut : m > 1 ? cut + v : 1.0;
+        s_cutoff[i] = m ? *cut_of(a, m, r, p) : 0.0;
+        s_left[i] = v;
       }
     }
   __syncthreads();
   const bool bad = s_bad;
-  if (tid >= 1 && tid <= q.k) {
-    const int p = parent_of(a, q, tid), x = cand_of(a, q, tid);
-    const bool in = x >= 0 && x < a.vocab;
-    s_parent[tid] = p;
-    s_cand[tid] = x;
-    const float l = in && !bad ? logit<BF>(a.target, (q.row0 + p) * a.t_stride + x) : -INFINITY;
-    const float dl = in && !bad && q.drow0 >= 0 ? logit<BF>(a.draft, (q.drow0 + p) * a.d_stride + x) : -INFINITY;
-    s_p[tid] = prob(l, s_max[0][p], q.c, s_log[0][p]);
-    s_q[tid] = q.drow0 >= 0 ? prob(dl, s_max[1][p], q.dc, s_log[1][p]) : 1.0;
-    if (a.logp)
-      a.logp[(size_t)r * (a.k + 1) + tid - 1] =
-          bad ? NAN : l > -INFINITY ? (float)((((double)l - (double)s_max[0][p]) * q.c - s_log[0][p]) * kLn2) : -INFINITY;
+  if (wave == 0) {
+    const bool siblings = drafted && a.max_children > 1 && cand;
+    const double cut = siblings ? s_cutoff[lane] : 0.0;
+    double mass = siblings ? s_left[lane] : 1.0;
+    double p = 0.0, qx = 1.0;
+    if (cand && !bad) {
+      p = prob(l, s_stat[0][parent], q.c);
+      if (drafted) qx = prob(dl, s_stat[1][parent], q.dc);
+    }
+    double left = drafted ? fmax(p - cut * qx, 0.0) : p;
+    if (lane < 32) s_cand[lane] = x;
+    uint32_t before = cand && !bad && !drafted ? s_children[parent] & ((1u << lane) - 1) : 0;
+    for (uint32_t b = before; b; b &= b - 1)   // a sibling that was rejected has taken the token
+      if (s_cand[__builtin_ctz(b)] == x) left = 0.0;
+    if (lane < 32) s_left[lane] = left;
+    if (!drafted) {
+      for (; before; before &= before - 1) mass -= s_left[__builtin_ctz(before)];
+      mass = fmax(mass, 0.0);
+    }
+    const bool yes = cand && !bad && (double)u * mass * qx < left;
+    const uint32_t accepted = (uint32_t)__ballot(yes);
+    if (lane < 32) s_cutoff[lane] = cut + mass;   // C once this child is rejected too
+    if (lane == 0) {
+      int at = 0, n = 0;
+      for (uint32_t next; !bad && (next = s_children[at] & accepted); ) {
+        at = __builtin_ctz(next);   // a child's row is past its parent's: the walk ends
+        s_path[n++] = at - 1;
+      }
+      const uint32_t tried = bad ? 0 : s_children[at];
+      s_at = at;
+      s_n = n;
+      s_cut = tried && drafted ? s_cutoff[31 - __builtin_clz(tried)] : 0.0;
+    }
   }
-  if (a.logp && tid > q.k && tid <= a.k) a.logp[(size_t)r * (a.k + 1) + tid - 1] = NAN;
+  if (wave == 1 && a.logp) {
+    if (lane <= q.k && !bad) s_log[lane] = log2(s_stat[0][lane].sum);
+    __builtin_amdgcn_wave_barrier();
+    if (writes && lane >= 1 && lane <= a.k)
+      a.logp[(size_t)r * (a.k + 1) + lane - 1] = bad || lane > q.k ? NAN : log_prob(l, s_stat[0][parent].top, s_log[parent], q.c);
+  }
   __syncthreads();
-  if (tid) return;
-  SampleDecision& d = a.dec[r];
-  int* path = a.reqs ? a.tree.path + q.row0 : a.path + (size_t)r * a.k;
-  int at = 0, n = 0, n_gone = 0;
-  double cut = 0.0, mass = 1.0;
-  if (!bad)
-    for (int i = 1; i <= q.k; ++i) {
-      if (s_parent[i] != at) continue;
-      double left;
-      if (q.drow0 >= 0) {
-        left = fmax(s_p[i] - cut * s_q[i], 0.0);
-      } else {
-        left = s_p[i];
-        for (int j = 0; j < n_gone; ++j)
-          if (d.gone[j] == s_cand[i]) left = 0.0;
-      }
-      if ((double)uniform_of(a, q, i) * mass * s_q[i] < left) {
-        path[n] = i - 1;
-        if (a.reqs) a.tree.host_path[q.row0 + n] = i - 1;
-        ++n;
-        at = i;
-        n_gone = 0;
-        cut = 0.0;
-        mass = 1.0;
-      } else if (q.drow0 >= 0) {
-        cut = s_cut[i];
-        mass = s_mass[i];
-      } else {
-        mass = fmax(mass - left, 0.0);
-        d.gone[n_gone++] = s_cand[i];
-      }
+  const int at = s_at, n = s_n;
+  if (writes) {
+    if (a.reqs) {
+      if (tid < n) a.tree.path[q.row0 + tid] = a.tree.host_path[q.row0 + tid] = s_path[tid];
+    } else {
+      if (tid < a.k) a.path[(size_t)r * a.k + tid] = tid < n ? s_path[tid] : -1;
+      if (tid == 0) a.accepted[r] = bad ? -1 : n;
     }
-  d.bad = bad;
-  d.accepted = bad ? -1 : n;
-  d.node = at;
-  d.n_gone = n_gone;
-  d.u = (double)uniform_of(a, q, 0);
-  d.cut = cut;
-  d.c = q.c;
-  d.dc = q.dc;
-  d.max = s_max[0][at];
-  d.log_sum = s_log[0][at];
-  d.draft = cut > 0.0;
-  d.dmax = cut > 0.0 ? s_max[1][at] : 0.f;
-  d.dlog_sum = cut > 0.0 ? s_log[1][at] : 0.0;
-  if (!a.reqs) {
-    for (int j = bad ? 0 : n; j < a.k; ++j) path[j] = -1;
-    a.accepted[r] = d.accepted;
   }
-}
-
-// What is left of each chunk at the node that gives the token, where a
-// drafter's distribution has been taken off.
-template <bool BF>
-__global__ __launch_bounds__(kThreads) void sample_left_kernel(const SampleArgs a) {
-  __shared__ double s_sum[4];
-  const int chunk = blockIdx.x, r = blockIdx.y;
-  const SampleDecision& d = a.dec[r];
-  if (d.bad || !d.draft) return;
-  const Req q = load_req(a, r);
-  const double left = chunk_left<BF>(a, (q.row0 + d.node) * a.t_stride, (q.drow0 + d.node) * a.d_stride, chunk, d.max, d.c,
-                                     d.log_sum, d.dmax, d.dc, d.dlog_sum, d.cut, s_sum);
-  if (threadIdx.x == 0) a.left[(size_t)r * a.chunks + chunk] = left;
-}
-
-// The token: the chunk in which the running sum passes u S, then the column.
-// One workgroup per request.
-template <bool BF>
-__global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs a) {
-  __shared__ double s_sum[4], s_run[kThreads];
-  __shared__ int s_chunk, s_tok, s_gone[32];
-  __shared__ double s_before;
-  const int r = blockIdx.x, tid = threadIdx.x;
-  const Req q = load_req(a, r);
-  const SampleDecision& d = a.dec[r];
-  int tok = -1;
-  if (!d.bad) {
-    const long long trow = (q.row0 + d.node) * a.t_stride, drow = d.draft ? (q.drow0 + d.node) * a.d_stride : 0;
-    const SamplePart* part = part_of(a, r, 0, d.node);
-    int n_gone = d.n_gone;
-    double cut = d.cut;
-    if (tid < n_gone) s_gone[tid] = d.gone[tid];
-    __syncthreads();
-    // this thread's columns of a chunk, in column order: a run of kPer, with what is left of each
-    auto values = [&](int chunk, double (&v)[kPer]) {
-      const int c0 = chunk * kSampleChunk + tid * kPer;
-      const double ps = exp2(-d.log_sum), qs = cut > 0.0 ? cut * exp2(-d.dlog_sum) : 0.0;
-      const float m = cut > 0.0 ? d.max : part[chunk].max;
-      const double scale = m > -INFINITY ? exp2(((double)m - (double)d.max) * d.c - d.log_sum) : 0.0;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const int col = c0 + e;
-        v[e] = 0.0;
-        if (col >= a.vocab || !(m > -INFINITY)) continue;
-        const float p = power(logit<BF>(a.target, trow + col), m, d.c);
-        v[e] = cut > 0.0 ? left_of(p, ps, power(logit<BF>(a.draft, drow + col), d.dmax, d.dc), qs) : (double)p * scale;
-        for (int j = 0; j < n_gone; ++j)
-          if (s_gone[j] == col) v[e] = 0.0;
-      }
-    };
-    auto chunk_sum = [&](int chunk) {
-      double v[kPer], s = 0.0;
-      values(chunk, v);
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) s += v[e];
-      return block_sum64(s, s_sum);
-    };
-    // what is left of chunk i; a chunk with a rejected token is summed again without it
-    auto left = [&](int i) {
-      if (cut > 0.0) return a.left[(size_t)r * a.chunks + i];
-      return part[i].max > -INFINITY ? part[i].sum * exp2(((double)part[i].max - (double)d.max) * d.c - d.log_sum) : 0.0;
-    };
-    __shared__ double s_again[32];
-    auto search = [&]() -> bool {   // false: nothing is left
-      for (int j = 0; j < n_gone; ++j) {
-        const double s = chunk_sum(min(max(s_gone[j], 0), a.vocab - 1) / kSampleChunk);
-        if (tid == 0) s_again[j] = s;
-      }
-      __syncthreads();
-      auto at = [&](int i) {
-        double v = left(i);
-        for (int j = 0; j < n_gone; ++j)
-          if (min(max(s_gone[j], 0), a.vocab - 1) / kSampleChunk == i) v = s_again[j];
-        return v;
-      };
-      // the first wave: 64 chunks at a time, running sums across lanes
-      if (tid < 64) {
-        double total = 0.0;
-        for (int i0 = 0; i0 < a.chunks; i0 += 64) total += wave_sum64(i0 + tid < a.chunks ? at(i0 + tid) : 0.0);
-        const double goal = d.u * total;
-        double before = 0.0;
-        int found = -1, last = -1;
-        double found_before = 0.0, last_before = 0.0;
-        for (int i0 = 0; i0 < a.chunks && found < 0; i0 += 64) {
-          const double v = i0 + tid < a.chunks ? at(i0 + tid) : 0.0;
-          double run = v;
-#pragma unroll
-          for (int o = 1; o < 64; o <<= 1) {
-            const double t = __shfl_up(run, o);
-            if (tid >= o) run += t;
-          }
-          const uint64_t hit = __ballot(v > 0.0 && before + run > goal), some = __ballot(v > 0.0);
-          if (some) {
-            const int w = 63 - __clzll((long long)some);
-            last = i0 + w;
-            last_before = before + __shfl(run - v, w);
-          }
-          if (hit) {
-            const int w = __ffsll((unsigned long long)hit) - 1;
-            found = i0 + w;
-            found_before = before + __shfl(run - v, w);
-          }
-          before += __shfl(run, 63);
-        }
-        if (tid == 0) {
-          s_chunk = found >= 0 ? found : last;
-          s_before = goal - (found >= 0 ? found_before : last_before);
-        }
-      }
-      __syncthreads();
-      return s_chunk >= 0;
-    };
-    bool some = search();
-    if (!some) {   // everything was taken off (a rounding: the candidate would have been accepted): the target's own
-      __syncthreads();
-      n_gone = 0;
-      cut = 0.0;
-      some = search();
-    }
-    const int chunk = max(s_chunk, 0);
-    double v[kPer], sum = 0.0;
-    values(chunk, v);
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) sum += v[e];
-    // running sums over the threads
-    s_run[tid] = sum;
-    if (tid == 0) s_tok = 0x7fffffff;
-    __syncthreads();
-    double run = sum;
-    {
-      const int lane = tid & 63;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double t = __shfl_up(run, o);
-        if (lane >= o) run += t;
-      }
-      if (lane == 63) s_sum[tid >> 6] = run;
-      __syncthreads();
-      for (int w = 0; w < (tid >> 6); ++w) run += s_sum[w];
-    }
-    double before = run - sum;
-    int mine = 0x7fffffff, last = -1;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      before += v[e];
-      if (v[e] > 0.0) {
-        if (before > s_before && mine == 0x7fffffff) mine = chunk * kSampleChunk + tid * kPer + e;
-        last = chunk * kSampleChunk + tid * kPer + e;
-      }
-    }
-    if (mine != 0x7fffffff) atomicMin(&s_tok, mine);
-    __syncthreads();
-    if (s_tok == 0x7fffffff) {   // the goal is the chunk's whole sum, up to rounding: its last column
-      __syncthreads();
-      if (tid == 0) s_tok = -1;
-      __syncthreads();
-      if (last >= 0) atomicMax(&s_tok, last);
-      __syncthreads();
-    }
-    tok = s_tok >= 0 ? s_tok : chunk * kSampleChunk;
+  double taken = s_cut;   // multiples of the drafter's distribution
+  if (bad || !(taken > 0.0)) {
+    if (!writes) return;
   }
-  if (tid) return;
-  float lp = NAN;
-  if (!d.bad) {
-    const float l = logit<BF>(a.target, (q.row0 + d.node) * a.t_stride + tok);
-    lp = (float)((((double)l - (double)d.max) * d.c - d.log_sum) * kLn2);
+  const RowStat t = s_stat[0][at];
+  const long long trow = (q.row0 + at) * a.t_stride, drow = drafted ? (q.drow0 + at) * a.d_stride : 0;
+  const double ps = 1.0 / t.sum;
+  RowStat d{};
+  double qs = 0.0;
+  if (taken > 0.0) {
+    d = s_stat[1][at];
+    qs = taken / d.sum;
+    double* out = a.left + (size_t)r * a.chunks;
+    for (int chunk = blockIdx.x * kWavesW + wave; chunk < a.chunks; chunk += gridDim.x * kWavesW) {
+      const double v = chunk_left<BF>(a, trow, drow, chunk, t.top, q.c, ps, d.top, q.dc, qs);
+      if (lane == 0) st<true>(out + chunk, v);
+    }
+    if (gridDim.x > 1) {
+      wait_vmem();
+      __syncthreads();
+      if (tid == 0) {
+        s_last = counter_add(a.ticket + r, 1) == (int)gridDim.x - 1;
+        if (s_last) st<true>(a.ticket + r, 0);   // ready for the next call
+      }
+      __syncthreads();
+      if (!s_last) return;
+    } else {
+      wait_vmem();
+      __syncthreads();
+    }
   }
-  if (a.reqs) {
-    const StepOut o{d.accepted, tok, d.bad, 0};
-    a.tree.sel[r] = o;
-    a.tree.host[r] = o;
-  } else {
+  // by the thread that has the token's logit
+  const auto give = [&](int tok, float y) {
+    if (a.reqs) {
+      const StepOut o{bad ? -1 : n, tok, bad, 0};
+      a.tree.sel[r] = o;
+      a.tree.host[r] = o;
+      return;
+    }
     a.token[r] = tok;
-    if (a.logp) a.logp[(size_t)r * (a.k + 1) + a.k] = lp;
+    if (a.logp) a.logp[(size_t)r * (a.k + 1) + a.k] = bad ? NAN : log_prob(y, t.top, s_log[at], q.c);
+  };
+  if (bad) {
+    if (tid == 0) give(-1, 0.f);
+    return;
+  }
+  {
+    const SamplePart* part = part_of(a, r, 0, at);
+    uint32_t gone = drafted ? 0 : s_children[at];   // rejected rows
+    const auto is_gone = [&](int col) {
+      bool g = false;
+      for (uint32_t b = gone; b; b &= b - 1) g |= s_cand[__builtin_ctz(b)] == col;
+      return g;
+    };
+    const auto chunk_of = [&](int row) {
+      const int c = s_cand[row];
+      return c >= 0 && c < a.vocab ? c / kSampleChunk : -1;
+    };
+    int chunk = -1;
+    double rest = 0.0;
+    for (int round = 0; round < 2 && chunk < 0; ++round) {
+      if (round) {   // nothing is left (a rounding: the last child would have been accepted): the target's own
+        taken = 0.0;
+        gone = 0;
+      }
+      // chunks of rejected tokens are summed again without them, a wave each
+      for (int i = wave; i <= q.k; i += kWavesW)
+        if (gone >> i & 1) {
+          const int ch = chunk_of(i);
+          double v = 0.0;
+          if (ch >= 0) {
+            float y[kPer];
+            load_chunk<BF>(a.target, trow, ch, a.vocab, y);
+            const double top = part[ch].top;
+            if (top > -INFINITY)
+#pragma unroll
+              for (int e = 0; e < kPer; ++e)
+                v += is_gone(ch * kSampleChunk + column<BF>(e)) ? 0.0 : (double)power(y[e], q.c, top);
+            v = wave_sum64(v);
+          }
+          if (lane == 0) s_again[i] = v;
+        }
+      __syncthreads();
+      const auto left = [&](int i) -> double {
+        if (taken > 0.0) return ld_coherent(a.left + (size_t)r * a.chunks + i);
+        const SamplePart p = part[i];
+        double v = p.sum;
+        for (uint32_t b = gone; b; b &= b - 1)
+          if (chunk_of(__builtin_ctz(b)) == i) v = s_again[__builtin_ctz(b)];
+        return v > 0.0 ? rescale(v, p.top, t.top) : 0.0;
+      };
+      // a run of chunks per thread (up to 1,048,576 tokens: one chunk)
+      const int per = (a.chunks + kWide - 1) / kWide;
+      double v = 0.0;
+      for (int i = tid * per; i < min((tid + 1) * per, a.chunks); ++i) v += left(i);
+      const int who = find_in_run(v, [&](double total) { return (double)u_tok * total; }, s_find, &rest);
+      chunk = who;
+      if (who >= 0 && per > 1) {
+        if (tid == who) {
+          int c = -1;
+          double goal = rest, at_c = 0.0;
+          for (int i = tid * per; i < min((tid + 1) * per, a.chunks); ++i) {
+            const double w = left(i);
+            if (!(w > 0.0)) continue;
+            c = i;
+            at_c = goal;
+            if (w > goal) break;
+            goal -= w;
+          }
+          s_at = c;
+          s_find.before = at_c;
+        }
+        __syncthreads();
+        chunk = s_at;
+        rest = s_find.before;
+      }
+    }
+    chunk = max(chunk, 0);
+    // the chunk's columns, one per thread: each summed as its chunk's sum took it
+    const int col = chunk * kSampleChunk + tid;
+    double v = 0.0;
+    float y = -INFINITY;
+    if (col < a.vocab) {
+      y = logit<BF>(a.target, trow + col);
+      if (taken > 0.0) {
+        v = left_of(power(y, q.c, t.top), ps, power(logit<BF>(a.draft, drow + col), q.dc, d.top), qs);
+      } else {
+        const double top = part[chunk].top;
+        if (top > -INFINITY && !is_gone(col)) v = rescale((double)power(y, q.c, top), top, t.top);
+      }
+    }
+    const int who = find_in_run(v, [&](double) { return rest; }, s_find, nullptr);
+    if (tid == max(who, 0)) give(min(col, a.vocab - 1), y);
   }
 }
 
-template <bool BF> hipError_t run(const SampleArgs& a, bool draft, int max_children, hipStream_t s) {
-  sample_stats_kernel<BF><<<dim3(a.chunks, a.k + 1, (draft ? 2 : 1) * a.n), kThreads, 0, s>>>(a);
+template <bool BF> hipError_t run(const SampleArgs& a, bool draft, hipStream_t s) {
+  static_assert(kSampleChunk == kWide, "the token's chunk: a column per thread");
+  const auto blocks = [&](int threads) { return (a.chunks + threads / 64 - 1) / (threads / 64); };
+  sample_stats_kernel<BF><<<dim3(blocks(kBlock), a.k + 1, (draft ? 2 : 1) * a.n), kBlock, 0, s>>>(a);
   if (draft)
-    for (int st = 1; st < max_children; ++st) sample_stage_kernel<BF><<<dim3(a.chunks, a.k + 1, a.n), kThreads, 0, s>>>(a, st);
-  sample_decide_kernel<BF><<<a.n, kThreads, 0, s>>>(a);
-  if (draft) sample_left_kernel<BF><<<dim3(a.chunks, a.n), kThreads, 0, s>>>(a);
-  sample_pick_kernel<BF><<<a.n, kThreads, 0, s>>>(a);
+    for (int st = 1; st < a.max_children; ++st)
+      sample_stage_kernel<BF><<<dim3(blocks(kWide), a.k + 1, a.n), kWide, 0, s>>>(a, st);
+  sample_finish_kernel<BF><<<dim3(draft ? blocks(kWide) : 1, a.n), kWide, 0, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_sample(const SampleArgs& a, bool draft, int max_children, hipStream_t s) {
+hipError_t launch_sample(const SampleArgs& a, bool draft, hipStream_t s) {
   if (a.n < 1 || a.k < 0 || a.k > 31 || a.vocab < 1 || a.chunks != (a.vocab + kSampleChunk - 1) / kSampleChunk || a.n > 32767)
     return hipErrorInvalidValue;
-  return a.bf16 ? run<true>(a, draft, max_children, s) : run<false>(a, draft, max_children, s);
+  return a.bf16 ? run<true>(a, draft, s) : run<false>(a, draft, s);
 }
 
 }  // namespace as2d

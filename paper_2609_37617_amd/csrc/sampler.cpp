@@ -3,7 +3,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <new>
@@ -75,8 +74,11 @@ int as2d_sampler_create(int32_t max_requests, int32_t max_k, int32_t max_vocab, 
   a.n = max_requests;
   a.k = max_k;
   a.chunks = (max_vocab + kSampleChunk - 1) / kSampleChunk;
+  a.max_children = max_k;
   hipError_t e = hipGetDevice(&s->dev);
-  if (e == hipSuccess) e = hipMalloc(&s->work, sample_layout(a, max_k, nullptr));
+  if (e == hipSuccess) e = hipMalloc(&s->work, sample_layout(a, max_requests, nullptr));
+  if (e == hipSuccess) e = hipMemset(s->work, 0, sizeof(int) * max_requests);
+  if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e == hipSuccess) e = hipEventCreateWithFlags(&s->ev, hipEventDisableTiming);
   if (e != hipSuccess) {
     const int rc = hip_fail(nullptr, "create", e);
@@ -110,9 +112,9 @@ int as2d_sampler_verify(as2d_sampler* s, const as2d_sample_args* p, void* hip_st
     return fail(s, AS2D_EINVAL, "sampler: null tensor");
   if (p->row_stride < vocab || (p->draft_logits && p->draft_row_stride < vocab))
     return fail(s, AS2D_EINVAL, "sampler: rows overlap (stride below %d)", vocab);
-  if ((!p->temperatures && (!(p->temperature > 0.0) || !std::isfinite(p->temperature))) || !(p->draft_temperature >= 0.0) ||
-      !std::isfinite(p->draft_temperature))
-    return fail(s, AS2D_EINVAL, "sampler: temperature %g, %g (> 0, and >= 0)", p->temperature, p->draft_temperature);
+  const auto good = [](double t) { return t >= kLeastTemp && t <= kMostTemp; };
+  if ((!p->temperatures && !good(p->temperature)) || (p->draft_temperature != 0.0 && !good(p->draft_temperature)))
+    return fail(s, AS2D_EINVAL, "sampler: temperature %g, of the drafter %g (1e-30 to 1e30)", p->temperature, p->draft_temperature);
   SampleArgs a{};
   int children[32] = {};
   for (int i = 1; i <= k; ++i) {
@@ -122,7 +124,7 @@ int as2d_sampler_verify(as2d_sampler* s, const as2d_sample_args* p, void* hip_st
     a.parent[i] = (signed char)(up + 1);
     ++children[up + 1];
   }
-  const int max_children = *std::max_element(children, children + 32);
+  a.max_children = *std::max_element(children, children + 32);
   a.target = p->logits;
   a.draft = k ? p->draft_logits : nullptr;
   a.t_stride = p->row_stride;
@@ -142,7 +144,7 @@ int as2d_sampler_verify(as2d_sampler* s, const as2d_sample_args* p, void* hip_st
   a.path = p->path;
   a.token = p->token;
   a.logp = p->logp;
-  sample_layout(a, max_children, (char*)s->work);
+  sample_layout(a, s->max_requests, (char*)s->work);
 
   OnDevice on(s->dev);
   hipStream_t st = (hipStream_t)hip_stream;
@@ -165,7 +167,7 @@ int as2d_sampler_verify(as2d_sampler* s, const as2d_sample_args* p, void* hip_st
   }
   s->used = true;
   s->last = st;
-  e = launch_sample(a, a.draft != nullptr, max_children, st);
+  e = launch_sample(a, a.draft != nullptr, st);
   return e == hipSuccess ? AS2D_OK : hip_fail(s, "launch", e);
 }
 

@@ -110,5 +110,5 @@ def test_the_binding_refuses_host_tensors(lib):
     import torch
     from paper_2609_37617_amd import as2d
     with pytest.raises(as2d.As2dError) as e:
-        as2d._on_device(torch.zeros(2), "q", "torch.float32", (2,))
+        as2d._on_device(torch.zeros(2), "q", torch.float32, (2,))
     assert e.value.code == as2d.EINVAL
