@@ -178,10 +178,10 @@ int as2d_verify_static(as2d_ctx* ctx, int32_t req, const int32_t* cands, int32_t
  * lowest-numbered child that equals its node's greedy token while there is
  * one.  out->accepted_len is the path's length, out->correction_token the
  * greedy token after its last row; path (optional, k entries) receives the
- * accepted candidates' numbers, then -1.  A chain gives what as2d_verify gives,
- * bit for bit.  Sibling candidates change the order of a row's attention sums
- * (hidden keys between the visible ones), so logits along a tree's path equal
- * a chain's to rounding.
+ * accepted candidates' numbers, then -1.  A call whose candidates are all chains
+ * gives what as2d_verify_batch gives, bit for bit; along a path of a tree,
+ * logits and cache rows are a chain's to rounding (the attention sums run in
+ * another order).
  *
  * as2d_verify_sampled: instead of comparing with greedy tokens, each node's
  * children are tested in order against the target's probabilities with given
@@ -233,8 +233,11 @@ int as2d_verify_tree_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const 
  * scores scaled by 1 / sqrt(head_dim).  q, out: [n_rows][n_q_heads][head_dim];
  * k, v: [n_rows][n_kv_heads][head_dim]; all in cfg->dtype, q and k already
  * rotated.  k and v are put into the layer's cache rows kv_len .. (kv_len stays
- * as it is, later calls overwrite them).  kv_len + n_rows <= max_kv_len (else
- * AS2D_ECAPACITY).  A pass of as2d_verify_tree runs the same kernels.
+ * as it is, later calls overwrite them; a row whose v is not finite is put as
+ * 0).  A row of k or v that holds a NaN or an infinity reaches only the rows
+ * that see it; such a v makes their whole head NaN.  kv_len + n_rows <=
+ * max_kv_len (else AS2D_ECAPACITY).  out must not overlap q, k or v.  Passes
+ * over trees run the same code on the rows of a pass.
  *
  * as2d_write_kv: keys (rotated) and values of positions pos .. pos + n_tok - 1
  * <= kv_len - 1 of the layer, [n_tok][n_kv_heads][head_dim] in `dtype`

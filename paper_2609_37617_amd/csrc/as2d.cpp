@@ -143,8 +143,6 @@ struct as2d_ctx {
   // operators on one cache layer (as2d_tree_attention, as2d_write_kv), which
   // return before they have run: the stream of the last one
   int dev = 0;
-  RowDesc* op_rows = nullptr;
-  ReqDesc* op_req = nullptr;
   hipEvent_t op_ev = nullptr;
   hipStream_t op_stream = nullptr;
   bool op_pending = false;
@@ -419,6 +417,11 @@ GemmArgs base_args(as2d_ctx* c, const GemmPlan& pl, const uint4* W, int M, const
 // kernels take base-2 exponentials of the scores).
 float attn_scale(int d) { return (float)(1.4426950408889634 / std::sqrt((double)d)); }
 
+// What a verification pass's rows are: as2d_verify's, or those of a call with a
+// path to walk (never through the persistent kernel): chains only, which take
+// as2d_verify's kernels and have its bits, or trees.
+enum PassRows { kPassVerify = 0, kPassChains = 1, kPassTrees = 2 };
+
 // Caches of up to 16 spans: the span kernel merges (no second launch).
 bool merge_last(int part_spans) { return part_spans <= 16; }
 
@@ -456,7 +459,7 @@ bool wave_tiles(const as2d_ctx* c, int M, const ReqDesc* reqs, int n, int part_s
 // attention key blocks of any request (it sizes the attention grid); tiles:
 // wave_tiles of the pass.
 int launch_pass(as2d_ctx* c, const PassBufs& B, int M, int n_att, int n_fin, int fin_rows, bool with_head,
-                int max_blocks, bool prefill, bool tiles, bool tree = false) {
+                int max_blocks, bool prefill, bool tiles, PassRows tree = kPassVerify) {
   const as2d_config& g = c->cfg;
   hipStream_t s = c->stream;
   const bool bf = c->bf16;
@@ -514,7 +517,7 @@ int launch_pass(as2d_ctx* c, const PassBufs& B, int M, int n_att, int n_fin, int
       a.out_plane = B.attn_plane;
       a.M = M;
       a.wave_tiles = tiles;
-      a.tree = tree;
+      a.tree = tree == kPassTrees;
       a.attn_rt = c->attn_rt;
       a.cus = c->grid_cus;
       Timed t(c, K_ATTN);
@@ -575,7 +578,7 @@ int launch_pass(as2d_ctx* c, const PassBufs& B, int M, int n_att, int n_fin, int
       HIP_TRY(c, launch_finish(B.d_rows, B.d_reqs + mr, n_fin, fin_rows, B.amax_val, B.amax_val2, B.amax_idx,
                                g.vocab / kPairCols, B.row_tok, B.row_bad, B.fin_counters,
                                HostOut{c->h_tok, c->h_margin, c->h_out}, s));
-      if (tree) HIP_TRY(c, launch_tree_walk(B.d_rows, B.d_reqs + mr, n_fin, B.row_tok, B.row_bad, c->tree, s));
+      if (tree != kPassVerify) HIP_TRY(c, launch_tree_walk(B.d_rows, B.d_reqs + mr, n_fin, B.row_tok, B.row_bad, c->tree, s));
     }
   }
   return AS2D_OK;
@@ -747,8 +750,8 @@ int launch_persistent(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows) {
 // arguments hold only pointers and sizes (the row and request descriptors
 // are read from device memory when the graph runs) and the attention grid
 // covers the slot capacity, so one graph (two with `tiles`, wave_tiles of the
-// pass, and two for passes over trees) serves every pass of that shape.
-int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persistent, bool tiles, bool tree,
+// pass, and as many for each of PassRows) serves every pass of that shape.
+int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persistent, bool tiles, PassRows tree,
               hipGraphExec_t* out) {
   const auto key = std::make_tuple((int)persistent, M, n_att, 4 * (int)tree + 2 * (int)tiles + c->keep_logits);
   auto it = c->graphs.find(key);
@@ -779,9 +782,8 @@ int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persi
 
 // One forward pass over the rows and requests in h_rows / h_reqs (see
 // launch_pass).  Verification passes run as a captured HIP graph (graph_for).
-// tree: the rows of trees of candidates (never the persistent kernel); `after`
-// launches what follows the pass before it is waited for.
-int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool verify_call = false, bool tree = false,
+// `after` launches what follows the pass before it is waited for.
+int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool verify_call = false, PassRows tree = kPassVerify,
                 const std::function<int()>& after = nullptr) {
   join_op(c);
   const as2d_config& g = c->cfg;
@@ -796,7 +798,7 @@ int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool v
   }
   if (max_blocks > c->n_blocks_cap) return fail(c, AS2D_ECAPACITY, "attention blocks %d > %d", max_blocks, c->n_blocks_cap);
   const bool verify_pass = verify_call && with_head && n_fin == n_att;
-  const bool persistent = verify_pass && !tree && c->exec_mode == AS2D_EXEC_PERSISTENT && c->pers_ok && c->pers_fit && M <= kStepRows;
+  const bool persistent = verify_pass && tree == kPassVerify && c->exec_mode == AS2D_EXEC_PERSISTENT && c->pers_ok && c->pers_fit && M <= kStepRows;
   const bool graph = verify_pass && c->exec_mode != AS2D_EXEC_EAGER && !c->timing;
   if (persistent && !step_layers_for(c, M)) return fail(c, AS2D_ENOMEM, "persistent step arguments");
   if (persistent || !verify_call) {   // the other passes read and write the host's arrays themselves
@@ -847,7 +849,7 @@ int as2d_prepare_graphs(as2d_ctx* c, int32_t max_rows) {
     for (const int kv_len : {M, std::max(M, c->cfg.max_kv_len)}) {
       const ReqDesc q{0, M, kv_len - M, 0};
       hipGraphExec_t ex = nullptr;
-      const int rc = graph_for(c, M, 1, 1, M, persistent, !persistent && wave_tiles(c, M, &q, 1, c->b.part_spans), false,
+      const int rc = graph_for(c, M, 1, 1, M, persistent, !persistent && wave_tiles(c, M, &q, 1, c->b.part_spans), kPassVerify,
                                &ex);
       if (rc) return rc;
     }
@@ -1019,9 +1021,10 @@ int tree_masks(as2d_ctx* c, const char* what, const int32_t* parents, int k, uin
 
 // The trees of a verification call, after assemble_verify: rotary positions,
 // masks and random numbers of its rows.  *max_k, *max_children: over the
-// requests; *draft: whether one has a drafter's logits.
+// requests; *draft: whether one has a drafter's logits; *chains: whether all
+// are chains.
 int assemble_tree(as2d_ctx* c, int n, const int32_t* parents, const int32_t* ks, const as2d_sampling* sampling, int* max_k,
-                  int* max_children, bool* draft) {
+                  int* max_children, bool* draft, bool* chains) {
   int off = 0;
   for (int r = 0; r < n; off += ks[r++]) {
     const int k = ks[r];
@@ -1033,6 +1036,7 @@ int assemble_tree(as2d_ctx* c, int n, const int32_t* parents, const int32_t* ks,
     for (int i = 0; i <= k; ++i) {
       rows[i].rot = c->h_reqs[r].L0 + depth[i];
       rows[i].mask = mask[i];
+      *chains &= depth[i] == i;
     }
     *max_k = std::max(*max_k, k);
     *max_children = std::max(*max_children, children);
@@ -1137,7 +1141,6 @@ PutRows layer_rows(const as2d_ctx* c, int req, int layer, int pos, const as2d_ro
   a.kv_cap = c->kv_stride;
   a.slot = req;
   a.pos0 = pos;
-  a.n_q = g.n_q_heads;
   a.n_kv = g.n_kv_heads;
   a.head_dim = g.head_dim;
   return a;
@@ -1520,8 +1523,6 @@ int as2d_load_weights(const as2d_config* cfg, const void* const* host, int32_t n
   CK(dalloc(c, &c->tree.sel, sizeof(StepOut) * g.max_requests));
   CK(dalloc(c, &c->tree.path, sizeof(int) * MR));
   CK(dalloc(c, &c->d_sreq, sizeof(SampleReq) * g.max_requests));
-  CK(dalloc(c, &c->op_rows, sizeof(RowDesc) * kStepRows));
-  CK(dalloc(c, &c->op_req, sizeof(ReqDesc)));
   HIP_TRY(c, hipEventCreateWithFlags(&c->op_ev, hipEventDisableTiming));
 
   // rotary table, evaluated in double precision: [pos][i] -> (cos, sin)
@@ -1680,13 +1681,13 @@ int as2d_verify_tree_batch(as2d_ctx* c, int32_t n, const int32_t* reqs, const in
   int rc = assemble_verify(c, n, reqs, cands, ks, outs, kMaxRows, &M);
   if (rc) return rc;
   OnDevice on(c->dev);
-  bool draft = false;
+  bool draft = false, chains = true;
   int max_children = 0, max_k = 0;
-  if ((rc = assemble_tree(c, n, parents, ks, sampling, &max_k, &max_children, &draft))) return rc;
+  if ((rc = assemble_tree(c, n, parents, ks, sampling, &max_k, &max_children, &draft, &chains))) return rc;
   if (sampling && (rc = upload_sampling(c, n, ks, parents, sampling, draft))) return rc;
   const int keep = c->keep_logits;
   if (sampling) c->keep_logits = 1;   // the pass writes the rows' logits
-  rc = run_forward(c, M, n, n, true, true, true, [&]() -> int {
+  rc = run_forward(c, M, n, n, true, true, chains ? kPassChains : kPassTrees, [&]() -> int {
     if (sampling) {
       const int rc = launch_sampling(c, n, max_k, max_children, draft);
       if (rc) return rc;
@@ -1734,26 +1735,26 @@ int as2d_tree_attention(as2d_ctx* c, int32_t req, int32_t layer, int32_t n_rows,
   if ((rc = check_rows(c, "tree_attention", q)) || (rc = check_rows(c, "tree_attention", k)) ||
       (rc = check_rows(c, "tree_attention", v)) || (rc = check_rows(c, "tree_attention", out)))
     return rc;
-  PutRows a = layer_rows(c, req, layer, st.kv_len, k, v);
-  if ((rc = tree_masks(c, "tree_attention", parents, n_rows - 1, a.mask, nullptr, nullptr))) return rc;
+  TreeOp op{};
+  if ((rc = tree_masks(c, "tree_attention", parents, n_rows - 1, op.mask, nullptr, nullptr))) return rc;
   OnDevice on(c->dev);
   hipStream_t s = (hipStream_t)hip_stream;
   if ((rc = begin_op(c, s))) return rc;
-  a.q = RowsView{q->data, q->row_stride, q->head_stride};
-  a.q_out = c->b.q;
-  a.rows = c->op_rows;
-  a.req = c->op_req;
-  HIP_TRY(c, launch_put_rows(c->bf16, c->bf16, a, n_rows, s));
+  const auto view = [](const as2d_rows* t) { return RowsView{t->data, t->row_stride, t->head_stride}; };
+  op.q = view(q);
+  op.k = view(k);
+  op.v = view(v);
+  op.out = view(out);
+  op.W = n_rows;
+  op.L0 = st.kv_len;
+  op.slot = req;
   const ReqDesc rq{0, n_rows, st.kv_len, req};
   const int blocks = (st.kv_len + n_rows + kAttnBlock - 1) / kAttnBlock, spans = (blocks + kAttnSpan - 1) / kAttnSpan;
   AttnArgs t{};
-  t.q = c->b.q;
-  t.k_cache = a.k_cache;
-  t.v_cache = a.v_cache;
+  t.k_cache = c->kc + (size_t)layer * c->layer_stride;
+  t.v_cache = c->vc + (size_t)layer * c->layer_stride;
   t.slot_stride = c->slot_stride;
   t.kv_cap = c->kv_stride;
-  t.rows = c->op_rows;
-  t.reqs = c->op_req;
   t.n_q = g.n_q_heads;
   t.n_kv = g.n_kv_heads;
   t.head_dim = g.head_dim;
@@ -1764,14 +1765,10 @@ int as2d_tree_attention(as2d_ctx* c, int32_t req, int32_t layer, int32_t n_rows,
   t.merge_last = merge_last(spans);
   t.attn_cnt = c->b.attn_cnt;
   t.M = n_rows;
-  t.tree = 1;
-  t.rows_out = out->data;
-  t.rows_out_row = out->row_stride;
-  t.rows_out_head = out->head_stride;
   t.wave_tiles = wave_tiles(c, n_rows, &rq, 1, spans);
   t.attn_rt = c->attn_rt;
   t.cus = c->grid_cus;
-  HIP_TRY(c, launch_attention(c->bf16, t, 1, blocks, false, s));
+  HIP_TRY(c, launch_tree_attention(c->bf16, t, op, blocks, s));
   return AS2D_OK;
 }
 

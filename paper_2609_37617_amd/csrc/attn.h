@@ -43,6 +43,11 @@
 
 namespace as2d {
 
+// What the rows of a verification pass see, and where they come from: a chain
+// of candidates, trees of them (RowDesc.mask), one tree's rows from tensors
+// (TreeOp).
+enum { kChain = 0, kTree = 1, kTreeOp = 2 };
+
 constexpr int kAttnChunk = kAttnSpanKeys / kWaves;   // keys of one wave's chunk of a span
 
 // 2^x by the hardware instruction (0 for x = -inf).
@@ -101,6 +106,17 @@ template <bool BF> __device__ __forceinline__ f4 mma3(const Op2& a, const Op2& b
   if constexpr (BF) {
     acc = mma_step<true>(a.h, b.h, acc);
     acc = mma_step<true>(a.h, b.l, acc);
+    acc = mma_step<true>(a.l, b.h, acc);
+  } else {
+    acc = mma_step<false>(a.h, b.h, acc);
+  }
+  return acc;
+}
+
+// The same where b's low part is 0 (values that are bf16).
+template <bool BF> __device__ __forceinline__ f4 mma2(const Op2& a, const Op2& b, f4 acc) {
+  if constexpr (BF) {
+    acc = mma_step<true>(a.h, b.h, acc);
     acc = mma_step<true>(a.l, b.h, acc);
   } else {
     acc = mma_step<false>(a.h, b.h, acc);
@@ -185,6 +201,93 @@ __device__ __forceinline__ void attn_load_q(const AttnArgs& p, const ReqDesc& rq
       v[0] = ldg(base + F::KE / 4 * ks);
       if constexpr (BF) v[1] = ldg(base + F::KE / 4 * ks + 1);
       q[rt][ks] = split_op<BF>(v);
+    }
+  }
+}
+
+// One tree's rows from tensors (kTreeOp): what every item of the kernel keeps
+// in LDS.  bad: rows whose values hold a NaN or an infinity; they are 0 in the
+// cache (a weight of 0 times them must stay 0) and every row that sees one
+// gets NaN.
+struct TreeLds {
+  uint32_t mask[32], bad;
+};
+
+// The rows' masks; the caller synchronises.
+__device__ __forceinline__ void tree_masks_to_lds(const TreeOp& op, TreeLds* t) {
+  const int i = threadIdx.x;
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) m = i == j ? op.mask[j] : m;   // (an index per lane would put the arguments in scratch)
+  if (i < 32) t->mask[i] = m;
+  if (i == 32) t->bad = 0;
+}
+
+// The rows' keys and values of KV head g into their cache rows, by the whole
+// workgroup (NT threads).  Every workgroup whose keys reach the rows does so
+// before it reads them: the same bytes each time, so that none waits for
+// another.
+template <bool BF, int D, int NT>
+__device__ __forceinline__ void tree_put(const AttnArgs& p, const TreeOp& op, int g, TreeLds* t) {
+  using T = typename ET<BF>::T;
+  constexpr int N = ET<BF>::PER16;   // elements of a thread's run
+  typedef T run __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  if (threadIdx.x == 0) t->bad = 0;
+  __syncthreads();
+  const size_t head = (size_t)op.slot * p.slot_stride + (size_t)g * p.kv_cap * D;   // float32 units
+  T* kb = reinterpret_cast<T*>(const_cast<float*>(p.k_cache) + head);
+  T* vb = reinterpret_cast<T*>(const_cast<float*>(p.v_cache) + head);
+  constexpr int kPer = 32 * (D / N) / NT > 0 ? 32 * (D / N) / NT : 1;
+  run k[kPer], v[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int i = (int)threadIdx.x + j * NT, r = i / (D / N), dd = i % (D / N) * N;
+    if (r < op.W) {
+      k[j] = *gmem(reinterpret_cast<const run*>(static_cast<const T*>(op.k.data) + r * op.k.row_stride + g * op.k.head_stride + dd));
+      v[j] = *gmem(reinterpret_cast<const run*>(static_cast<const T*>(op.v.data) + r * op.v.row_stride + g * op.v.head_stride + dd));
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int i = (int)threadIdx.x + j * NT, r = i / (D / N), dd = i % (D / N) * N;
+    if (r >= op.W) continue;
+    const int pos = op.L0 + r;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if (!(fabsf(to_f(v[j][e])) < INFINITY)) {
+        bad = true;
+        v[j][e] = T(0);
+      }
+      *gmem(vb + v_elem(pos, 0, dd + e, D, BF)) = v[j][e];
+      if constexpr (BF) *gmem(vb + v_elem(pos, 1, dd + e, D, BF)) = T(0);
+    }
+    if (bad) atomicOr(&t->bad, 1u << r);
+    T* kr = kb + (size_t)pos * (BF ? 2 : 1) * D + dd;
+    *gmem(reinterpret_cast<u32x4*>(kr)) = __builtin_bit_cast(u32x4, k[j]);
+    if constexpr (BF) *gmem(reinterpret_cast<u32x4*>(kr + D)) = u32x4{0, 0, 0, 0};
+  }
+  wait_vmem();
+  __syncthreads();   // this workgroup's rows are in its caches
+}
+
+// The operands of a block's queries as attn_load_q, from the tensor: bf16
+// values have no low part.
+template <bool BF, int D, int RT>
+__device__ __forceinline__ void tree_load_q(const TreeOp& op, const AttnRows& rows, Op2 (&q)[RT][D / AttnFmt<BF>::KE]) {
+  using F = AttnFmt<BF>;
+  using T = typename ET<BF>::T;
+  typedef T run __attribute__((ext_vector_type(F::PER), aligned(sizeof(T))));
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int rr = 16 * rt + (lane & 15);
+    const T* base = static_cast<const T*>(op.q.data) + rows.row(rr) * op.q.row_stride + rows.head(rr) * op.q.head_stride +
+                    F::PER * (lane >> 4);
+#pragma unroll
+    for (int ks = 0; ks < D / F::KE; ++ks) {
+      q[rt][ks].h = __builtin_bit_cast(uint4, *gmem(reinterpret_cast<const run*>(base + F::KE * ks)));
+      q[rt][ks].l = make_uint4(0, 0, 0, 0);
     }
   }
 }
@@ -359,10 +462,10 @@ __device__ __forceinline__ void attn_state_merge(AttnState<RT, DTW>& st, const f
 struct NoOp {
   __device__ void operator()() const {}
 };
-template <bool BF, int D, int RT, bool TREE = false, class PreV = NoOp>
+template <bool BF, int D, int RT, int TREE = kChain, class PreV = NoOp>
 __device__ __forceinline__ void attn_span_chunks(const AttnArgs& p, const ReqDesc& rq, const AttnRows& rows, int sp,
                                                  const Op2 (&q)[RT][D / AttnFmt<BF>::KE], const AttnRaw<BF, D>& raw,
-                                                 unsigned char* smem, PreV pre_v = PreV{}) {
+                                                 unsigned char* smem, PreV pre_v = PreV{}, const TreeLds* tree = nullptr) {
 #pragma clang fp contract(off)
   using Raw = AttnRaw<BF, D>;
   constexpr int KS = Raw::KS, DT = Raw::DT, DTW = D / 64, R = 16 * RT;
@@ -385,12 +488,15 @@ __device__ __forceinline__ void attn_span_chunks(const AttnArgs& p, const ReqDes
     const int pos = rq.L0 + rows.row(16 * rt + lr);
     // a chunk that reaches the tree's rows (wave-uniform); the other chunks' keys all precede them
     const bool in_tree = TREE && kc + kAttnChunk > rq.L0;
-    const uint32_t mask = in_tree ? ldg(&p.rows[rq.row_start + pos - rq.L0].mask) : 0;
+    const uint32_t mask = !in_tree ? 0 : TREE == kTreeOp ? tree->mask[pos - rq.L0] : ldg(&p.rows[rq.row_start + pos - rq.L0].mask);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       f4 acc = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) acc = mma3<BF>(raw.k[kt][ks], q[rt][ks], acc);
+      for (int ks = 0; ks < KS; ++ks) {
+        if constexpr (TREE == kTreeOp) acc = mma2<BF>(raw.k[kt][ks], q[rt][ks], acc);
+        else acc = mma3<BF>(raw.k[kt][ks], q[rt][ks], acc);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int key = kc + 16 * kt + 4 * lg + i;
@@ -415,6 +521,8 @@ __device__ __forceinline__ void attn_span_chunks(const AttnArgs& p, const ReqDes
     float sm = (((pj[0][0] + pj[0][1]) + pj[0][2]) + pj[0][3]) + (((pj[1][0] + pj[1][1]) + pj[1][2]) + pj[1][3]);
     sm = swap_combine<false>(sm, FAdd{});
     sm = swap_combine<true>(sm, FAdd{});
+    if constexpr (TREE == kTreeOp)
+      if (kc + kAttnChunk > rq.L0 && (tree->mask[rows.row(16 * rt + lr)] & tree->bad)) sm = NAN;
     if (lg == 0) {
       SM[wave * R + 16 * rt + lr] = mx;
       SL[wave * R + 16 * rt + lr] = sm;
@@ -492,11 +600,12 @@ __device__ __forceinline__ void attn_merge_chunks(unsigned char* smem, AttnState
   }
 }
 
-template <bool BF, int D, int RT, bool TREE = false>
+template <bool BF, int D, int RT, int TREE = kChain>
 __device__ __forceinline__ void attn_span_state(const AttnArgs& p, const ReqDesc& rq, const AttnRows& rows, int sp,
                                                 const Op2 (&q)[RT][D / AttnFmt<BF>::KE], const AttnRaw<BF, D>& raw,
-                                                unsigned char* smem, AttnState<RT, D / 64>& st) {
-  attn_span_chunks<BF, D, RT, TREE>(p, rq, rows, sp, q, raw, smem);
+                                                unsigned char* smem, AttnState<RT, D / 64>& st,
+                                                const TreeLds* tree = nullptr) {
+  attn_span_chunks<BF, D, RT, TREE>(p, rq, rows, sp, q, raw, smem, NoOp{}, tree);
   attn_merge_chunks<BF, D, RT>(smem, st);
 }
 
@@ -538,28 +647,22 @@ __device__ __forceinline__ void attn_store_span(const AttnArgs& p, const ReqDesc
 }
 
 // The attention output of a row: N consecutive dimensions from n = h D + dim.
-// A tree pass may ask for rows of the model's type (rows_out, any strides and
-// element alignment); the next GEMM takes activation planes.
-template <bool BF, int D, bool OUT_COH, bool TREE, int N>
-__device__ __forceinline__ void attn_store_out(const AttnArgs& p, int row, int n, const float* o) {
-  if constexpr (TREE)
-    if (p.rows_out) {
-      const size_t at = (size_t)row * p.rows_out_row + (size_t)(n / D) * p.rows_out_head + n % D;
-      if constexpr (BF) {
-        typedef uint16_t run __attribute__((ext_vector_type(N), aligned(2)));
-        run v;
+// A pass's next GEMM takes activation planes; a tree's rows from tensors go to
+// its output tensor (any strides, so runs of the element's alignment).
+template <bool BF, int D, bool OUT_COH, int N>
+__device__ __forceinline__ void attn_store_out(const AttnArgs& p, const TreeOp* op, int row, int n, const float* o) {
+  if (op) {
+    using T = typename ET<BF>::T;
+    typedef T run __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    run v;
 #pragma unroll
-        for (int t = 0; t < N; ++t) v[t] = f2bf(o[t]);
-        *gmem(reinterpret_cast<run*>(static_cast<uint16_t*>(p.rows_out) + at)) = v;
-      } else {
-        typedef float run __attribute__((ext_vector_type(N), aligned(4)));
-        run v;
-#pragma unroll
-        for (int t = 0; t < N; ++t) v[t] = o[t];
-        *gmem(reinterpret_cast<run*>(static_cast<float*>(p.rows_out) + at)) = v;
-      }
-      return;
-    }
+    for (int t = 0; t < N; ++t)
+      if constexpr (BF) v[t] = f2bf(o[t]);
+      else v[t] = o[t];
+    T* out = static_cast<T*>(const_cast<void*>(op->out.data)) + row * op->out.row_stride + n / D * op->out.head_stride + n % D;
+    *gmem(reinterpret_cast<run*>(out)) = v;
+    return;
+  }
   const size_t e = frag_index<BF>(row, n, p.n_q * D);
   if constexpr (N == 1) store_act<BF, OUT_COH>(p.out, p.out_plane, e, o[0]);
   else store_act_run<BF, OUT_COH, N>(p.out, p.out_plane, e, o);
@@ -570,8 +673,8 @@ __device__ __forceinline__ void attn_store_out(const AttnArgs& p, int row, int n
 // wave (lane l % 16 holds dimensions [DQ (l % 16), DQ (l % 16) + DQ),
 // DQ = D / 16); writes the attention output planes (OUT_COH: with
 // agent-scope stores).
-template <bool BF, int D, bool OUT_COH, bool TREE = false>
-__device__ __forceinline__ void attn_merge_row(const AttnArgs& p, const ReqDesc& rq, int r, int h) {
+template <bool BF, int D, bool OUT_COH>
+__device__ __forceinline__ void attn_merge_row(const AttnArgs& p, const ReqDesc& rq, int r, int h, const TreeOp* op = nullptr) {
   constexpr int DQ = D / 16;   // dimensions per lane
   constexpr int kB = 8;        // spans whose loads are in flight together
   static_assert(DQ % 4 == 0, "whole 16-byte reads per lane");
@@ -631,7 +734,7 @@ __device__ __forceinline__ void attn_merge_row(const AttnArgs& p, const ReqDesc&
   float o[DQ];
 #pragma unroll
   for (int t = 0; t < DQ; ++t) o[t] = A[t] / L;
-  attn_store_out<BF, D, OUT_COH, TREE, DQ>(p, row, h * D + DQ * ql, o);
+  attn_store_out<BF, D, OUT_COH, DQ>(p, op, row, h * D + DQ * ql, o);
 }
 
 // Row i of request rq, head h, by one wave: the same fold as attn_merge_row
@@ -642,15 +745,18 @@ __device__ __forceinline__ void attn_merge_row(const AttnArgs& p, const ReqDesc&
 // running maximum before span s is the maximum of m over spans 0 .. s - 1,
 // which a prefix scan gives exactly (fmax rounds nothing).  The states were
 // stored by an earlier kernel; the output planes are read by a later one.
-template <bool BF, int D, bool TREE = false>
-__device__ __forceinline__ void attn_merge_wave(const AttnArgs& p, const ReqDesc& rq, int i, int h) {
+// runs: states of that many runs instead of spans (attn_tree.hip; the first
+// run's has a maximum, later ones may be empty).
+template <bool BF, int D>
+__device__ __forceinline__ void attn_merge_wave(const AttnArgs& p, const ReqDesc& rq, int i, int h, const TreeOp* op = nullptr,
+                                                int runs = 0) {
 #pragma clang fp contract(off)
   constexpr int DL = D / 64;   // dimensions per lane
   constexpr int kB = 16;       // spans per batch
   static_assert(DL == 1 || DL == 2, "64 or 128 dimensions");
   const int lane = threadIdx.x & 63, bl = lane & (kB - 1);
   const int row = rq.row_start + i;
-  const int ns = (rq.L0 + i) / kAttnSpanKeys + 1;
+  const int ns = runs ? runs : (rq.L0 + i) / kAttnSpanKeys + 1;
   auto at = [&](int sp) { return ((size_t)row * p.n_q + h) * p.part_spans + sp; };
   struct Batch {
     float m, l, a[kB][DL];
@@ -715,7 +821,7 @@ __device__ __forceinline__ void attn_merge_wave(const AttnArgs& p, const ReqDesc
   float o[DL];
 #pragma unroll
   for (int t = 0; t < DL; ++t) o[t] = A[t] / L;
-  attn_store_out<BF, D, false, TREE, DL>(p, row, h * D + DL * lane, o);
+  attn_store_out<BF, D, false, DL>(p, op, row, h * D + DL * lane, o);
 }
 
 }  // namespace as2d

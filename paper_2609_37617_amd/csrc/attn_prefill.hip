@@ -55,14 +55,11 @@ __device__ __forceinline__ MergeCoef attn_coef0(float& M, float& L, float m, flo
 // NW waves' row tiles.  This lane's row sits at position pos and its queries
 // come from load_q once the first keys are requested; p0: a position no row
 // of the tile is before; last: the last key any of the workgroup's rows sees.
-// TREE: the rows of one request's tree of candidates, this lane's mask in
-// `mask` (p0: the committed length, the root's row, which every row sees).
 // on_span(span, M, S, A) gets each span's state: A[t][i] is dimension
 // 16 t + 4 (lane / 16) + i.  Ends with the workgroup's barrier.
-template <int D, int NW, bool TREE, class LoadQ, class OnSpan>
+template <int D, int NW, class LoadQ, class OnSpan>
 __device__ __forceinline__ void attn_walk(const AttnArgs& p, const ReqDesc& rq, int g, int p0, int pos, int last,
-                                          uint32_t mask, int c_first, int c_end, unsigned char* smem, LoadQ&& load_q,
-                                          OnSpan&& on_span) {
+                                          int c_first, int c_end, unsigned char* smem, LoadQ&& load_q, OnSpan&& on_span) {
 #pragma clang fp contract(off)
   constexpr int KS = D / 32, DT = D / 16, U = attn_wide_units<D>(), NV = U / (64 * NW);
   constexpr int KU = D / 4;   // units of a key: hi, lo
@@ -174,10 +171,8 @@ __device__ __forceinline__ void attn_walk(const AttnArgs& p, const ReqDesc& rq, 
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = kc + 16 * kt + 4 * lg + i;
-          if (TREE ? !tree_sees(mask, key, p0, pos) : key > pos) sa[kt][i] = -INFINITY;
-        }
+        for (int i = 0; i < 4; ++i)
+          if (kc + 16 * kt + 4 * lg + i > pos) sa[kt][i] = -INFINITY;
     }
     float s[2][4];
 #pragma unroll
@@ -299,8 +294,8 @@ __global__ __launch_bounds__(64 * kPrefillWaves, 2) void attn_prefill_wide_kerne
 #pragma unroll
     for (int i = 0; i < 4; ++i) A[t][i] = 0.f;
   const int row = rq.row_start + pos - rq.L0;
-  attn_walk<D, kPrefillWaves, false>(
-      p, rq, g, p0, pos, last_all, 0, 0, last_all / kAttnChunk + 1, smem, [&](Op2(&q)[D / 32]) { attn_load_row<D>(p, row, h, q); },
+  attn_walk<D, kPrefillWaves>(
+      p, rq, g, p0, pos, last_all, 0, last_all / kAttnChunk + 1, smem, [&](Op2(&q)[D / 32]) { attn_load_row<D>(p, row, h, q); },
       [&](int, float Ms, float Ss, const float(&As)[DT][4]) {
         // a row that does not reach the span: unchanged
         const MergeCoef ka = attn_coef0(M, S, Ms, Ss);
@@ -326,7 +321,7 @@ __global__ __launch_bounds__(64 * kPrefillWaves, 2) void attn_prefill_wide_kerne
 // span needs no exchange between waves (attn_group2_kernel: once per 16
 // rows, its four waves meeting twice per span).  Span states go to memory
 // for attn_merge_kernel.  A fixed grid takes the items in turn.
-template <int D, bool TREE>
+template <int D>
 __global__ __launch_bounds__(64 * kSpanWaves, 2) void attn_spans_wide_kernel(const AttnArgs p, int n_reqs) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int DT = D / 16, kRows = 16 * kSpanWaves, kChunks = kAttnSpanKeys / kAttnChunk;
@@ -348,9 +343,8 @@ __global__ __launch_bounds__(64 * kSpanWaves, 2) void attn_spans_wide_kernel(con
     const int rr = 16 * wave + lr, i = rows.row(rr), h = rows.head(rr), row = rq.row_start + i;
     const int last = rq.L0 + rq.W - 1, pos = rq.L0 + i;
     const int c_first = j * R * kChunks, c_end = min(c_first + R * kChunks, last / kAttnChunk + 1);
-    const uint32_t mask = TREE ? ldg(&p.rows[row].mask) : 0;
-    attn_walk<D, kSpanWaves, TREE>(
-        p, rq, g, rq.L0, pos, last, mask, c_first, c_end, smem, [&](Op2(&q)[D / 32]) { attn_load_row<D>(p, row, h, q); },
+    attn_walk<D, kSpanWaves>(
+        p, rq, g, rq.L0, pos, last, c_first, c_end, smem, [&](Op2(&q)[D / 32]) { attn_load_row<D>(p, row, h, q); },
         [&](int sp, float Ms, float Ss, const float(&As)[DT][4]) {
           if (!rows.valid(rr) || pos < sp * kAttnSpanKeys) return;
           const size_t o = ((size_t)row * p.n_q + h) * p.part_spans + sp;
@@ -366,20 +360,14 @@ hipError_t prepare_attn_prefill() {
   auto allow = [](const void* k) {
     return hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, attn_wide_lds_bytes<128>());
   };
-  hipError_t e = allow(reinterpret_cast<const void*>(&attn_prefill_wide_kernel<128>));
-  if (e == hipSuccess) e = allow(reinterpret_cast<const void*>(&attn_spans_wide_kernel<128, false>));
-  return e == hipSuccess ? allow(reinterpret_cast<const void*>(&attn_spans_wide_kernel<128, true>)) : e;
+  const hipError_t e = allow(reinterpret_cast<const void*>(&attn_prefill_wide_kernel<128>));
+  return e == hipSuccess ? allow(reinterpret_cast<const void*>(&attn_spans_wide_kernel<128>)) : e;
 }
 
 hipError_t launch_attn_spans(const AttnArgs& a, int n_reqs, int grid, hipStream_t s) {
-  const auto run = [&](auto tree) {
-    constexpr bool T = decltype(tree)::value;
-    if (a.head_dim == 128) attn_spans_wide_kernel<128, T><<<grid, 64 * kSpanWaves, attn_wide_lds_bytes<128>(), s>>>(a, n_reqs);
-    else attn_spans_wide_kernel<64, T><<<grid, 64 * kSpanWaves, attn_wide_lds_bytes<64>(), s>>>(a, n_reqs);
-  };
-  if (a.head_dim != 128 && a.head_dim != 64) return hipErrorInvalidValue;
-  if (a.tree) run(std::true_type{});
-  else run(std::false_type{});
+  if (a.head_dim == 128) attn_spans_wide_kernel<128><<<grid, 64 * kSpanWaves, attn_wide_lds_bytes<128>(), s>>>(a, n_reqs);
+  else if (a.head_dim == 64) attn_spans_wide_kernel<64><<<grid, 64 * kSpanWaves, attn_wide_lds_bytes<64>(), s>>>(a, n_reqs);
+  else return hipErrorInvalidValue;
   return hipGetLastError();
 }
 

@@ -415,6 +415,19 @@ __device__ __forceinline__ void attn_run_length(const ReqDesc* reqs, int n_reqs,
   while (total > G && total > least) total = n_items(++R);
 }
 
+// The same of one request.
+template <class Items, class Groups>
+__device__ __forceinline__ void run_length_of(const ReqDesc& rq, int G, Items&& items, Groups&& groups, int& R, int& total) {
+  R = 1;
+  total = items(rq, 1);
+  if (total <= G) return;
+  const int least = groups(rq);
+  R = (total + G - 1) / G;
+  total = items(rq, R);
+  while (total > G && total > least) total = items(rq, ++R);
+}
+__device__ __forceinline__ ReqDesc tree_req(const TreeOp& op) { return ReqDesc{0, op.W, op.L0, op.slot}; }
+
 // Workgroups are dealt to the 8 XCDs round-robin by linear index.  The
 // index v of the work a block takes: XCD j's blocks take one contiguous
 // range of v (the first n % 8 XCDs one more each), in dispatch order.

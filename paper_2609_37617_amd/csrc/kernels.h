@@ -164,6 +164,22 @@ __host__ __device__ inline size_t v_elem(int pos, int part, int dd, int d, bool 
   return ((size_t)(pos >> 5) * parts + part) * d * 32 + (size_t)dd * 32 + col;
 }
 
+// Rows [n][heads][head_dim] of a device tensor, dimensions adjacent, strides in
+// elements.
+struct RowsView {
+  const void* data;
+  long long row_stride, head_stride;
+};
+
+// Attention of a tree's rows over one layer of a request's cache, from device
+// tensors of the model's type (no pass around it): W rows at cache rows L0 ..,
+// which row sees which in mask.
+struct TreeOp {
+  RowsView q, k, v, out;
+  int W, L0, slot;
+  uint32_t mask[32];
+};
+
 struct AttnArgs {
   const float* q;        // [M][n_q*d]
   const float* k_cache;  // this layer
@@ -185,8 +201,6 @@ struct AttnArgs {
   long long out_plane;
   int M;
   int tree;              // verification passes: rows see the committed keys and the request's rows in their mask
-  void* rows_out;        // tree: the output as rows of the model's type instead of the planes
-  long long rows_out_row, rows_out_head;   // its strides, in elements
   int wave_tiles;        // verification passes of bf16 models: a row tile per wave (attn_spans_wide_kernel)
   int attn_rt;           // row tiles per block of the verification kernel (0: chosen per launch)
   int cus;               // compute units the verification kernels may fill (the CU budget)
@@ -264,6 +278,14 @@ hipError_t launch_step(bool bf16, int MT, int head_dim, int sl, const StepArgs& 
 // sizes the grid (any value covers every cache length; the grid is at most
 // kAttnGrid workgroups).  prefill: one request, its rows in order.
 hipError_t launch_attention(bool bf16, const AttnArgs& a, int n_reqs, int max_blocks, bool prefill, hipStream_t s);
+// The same of one tree's rows from tensors (a: the cache, the states' buffers and the
+// grid's limits); blocks: 64-key blocks of its keys.
+hipError_t launch_tree_attention(bool bf16, const AttnArgs& a, const TreeOp& op, int blocks, hipStream_t s);
+// Trees of bf16 models over long caches (attn_tree.hip), `grid` workgroups: one tree's
+// rows from tensors, or a pass's requests.
+hipError_t launch_tree_op(const AttnArgs& a, const TreeOp& op, int grid, hipStream_t s);
+hipError_t launch_tree_pass(const AttnArgs& a, int n_reqs, int grid, hipStream_t s);
+hipError_t prepare_tree();
 // The prefill pass of a bf16 model (attn_prefill.hip): one request of a.M rows.
 hipError_t launch_attn_prefill(const AttnArgs& a, hipStream_t s);
 hipError_t prepare_attn_prefill();
@@ -277,27 +299,17 @@ hipError_t launch_finish(const RowDesc* rows, const ReqDesc* reqs, int n_reqs, i
                          const float* amax_val, const float* amax_val2, const int* amax_idx, int n_pairs,
                          int* row_tok, int* row_bad, int* counters, const HostOut& out, hipStream_t s);
 
-// Passes over trees (tree.hip).  Rows [n][heads][head_dim] of a device
-// tensor, dimensions adjacent, strides in elements.
-struct RowsView {
-  const void* data;
-  long long row_stride, head_stride;
-};
-// Rows into cache rows pos0 .. of one layer and, with q_out, the queries and
-// descriptors of a tree attention.
+// Rows into cache rows pos0 .. of one layer (tree.hip).
 struct PutRows {
-  RowsView q, k, v;
+  RowsView k, v;
   float *k_cache, *v_cache;   // this layer
   long long slot_stride;
-  int kv_cap, slot, pos0, n_q, n_kv, head_dim;
-  float* q_out;               // [n][n_q * head_dim], or null: only the cache is written
-  RowDesc* rows;
-  ReqDesc* req;
-  uint32_t mask[32];
+  int kv_cap, slot, pos0, n_kv, head_dim;
 };
-// src_bf16: the type of q, k and v.
+// src_bf16: the type of k and v.
 hipError_t launch_put_rows(bool bf16, bool src_bf16, const PutRows& a, int n, hipStream_t s);
 
+// Passes over trees (tree.hip).
 // Outcome of a pass over trees, on the device and in pinned host memory:
 // per request (accepted -1: non-finite), and the accepted candidates from
 // the request's first row on.

@@ -319,8 +319,10 @@ hipError_t launch_gemm(bool bf16, int amode, int epi, const GemmArgs& a, hipStre
 // The items of a launch with blocks of RT row tiles.  LOWREG (RT = 1): a
 // workgroup within half the register file (two per compute unit), one span
 // buffer, the values fetched once the span's scores are formed.
-template <bool BF, int D, int RT, bool TREE, bool LOWREG = false>
-__device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, unsigned char* smem) {
+// TREE kTreeOp: one tree's rows from tensors (op, its rows' masks in tree).
+template <bool BF, int D, int RT, int TREE, bool LOWREG = false>
+__device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, unsigned char* smem, const TreeOp* op = nullptr,
+                                                 TreeLds* tree = nullptr) {
   static_assert(!LOWREG || RT == 1, "one row tile");
   constexpr int KS = D / AttnFmt<BF>::KE;
   constexpr int BR = 16 * RT;   // rows of a block
@@ -335,27 +337,37 @@ __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, 
     return p.n_kv * blocks(rq) * ((ns + R - 1) / R);
   };
   int R, total;
-  attn_run_length(p.reqs, n_reqs, G, items, [&](const ReqDesc& rq) { return p.n_kv * blocks(rq); }, R, total);
+  const auto groups = [&](const ReqDesc& rq) { return p.n_kv * blocks(rq); };
+  if constexpr (TREE == kTreeOp) run_length_of(tree_req(*op), G, items, groups, R, total);
+  else attn_run_length(p.reqs, n_reqs, G, items, groups, R, total);
   for (int t = xcd_contiguous(blockIdx.x, G); t < total; t += G) {
     // item t: request r, then run j, KV head g, row block b
-    int u = t;
-    const int r = n_reqs == 1 ? 0 : find_request(p.reqs, n_reqs, u, [&](const ReqDesc& q) { return items(q, R); });
-    const ReqDesc rq = load_invariant(p.reqs + r);
+    int u = t, r = 0;
+    ReqDesc rq;
+    if constexpr (TREE == kTreeOp) {
+      rq = tree_req(*op);
+    } else {
+      if (n_reqs > 1) r = find_request(p.reqs, n_reqs, u, [&](const ReqDesc& q) { return items(q, R); });
+      rq = load_invariant(p.reqs + r);
+    }
     const int ns = (rq.L0 + rq.W - 1) / kAttnSpanKeys + 1, nb = blocks(rq);
     const int j = u / (p.n_kv * nb);
     const int v = u - j * p.n_kv * nb;
     const int g = v / nb, b = v - g * nb;
     const AttnRows rows{g * hpg, rq.W, hpg * rq.W, b * BR};
     const int sp0 = j * R, sp1 = min(sp0 + R, ns);
+    if constexpr (TREE == kTreeOp)
+      if (sp1 * kAttnSpanKeys > rq.L0) tree_put<BF, D, 256>(p, *op, g, tree);
     // the first span's keys and values, then the queries, all in flight at once
     AttnRaw<BF, D> ka;
     if constexpr (LOWREG) attn_fetch_k<BF, D>(p, rq, g, sp0, ka);
     else attn_fetch<BF, D>(p, rq, g, sp0, ka);
     Op2 q[RT][KS];
-    attn_load_q<BF, D, RT>(p, rq, rows, q);
+    if constexpr (TREE == kTreeOp) tree_load_q<BF, D, RT>(*op, rows, q);
+    else attn_load_q<BF, D, RT>(p, rq, rows, q);
     auto run = [&](int sp, const AttnRaw<BF, D>& raw) {
       AttnState<RT, D / 64> state;
-      attn_span_state<BF, D, RT, TREE>(p, rq, rows, sp, q, raw, smem, state);
+      attn_span_state<BF, D, RT, TREE>(p, rq, rows, sp, q, raw, smem, state, tree);
       attn_store_span<D, RT>(p, rq, rows, sp, state);
       lds_sync();   // the LDS is written again next (a prefetch stays in flight)
     };
@@ -367,7 +379,7 @@ __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, 
         attn_span_chunks<BF, D, 1, TREE>(p, rq, rows, sp, q, ka, smem, [&] {
           attn_fetch_v<BF, D>(p, rq, g, sp, ka);
           if (sp + 1 < sp1) attn_fetch_k<BF, D>(p, rq, g, sp + 1, ka);
-        });
+        }, tree);
         attn_merge_chunks<BF, D, 1>(smem, state);
         attn_store_span<D, 1>(p, rq, rows, sp, state);
         lds_sync();   // the LDS is written again next
@@ -404,7 +416,7 @@ __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, 
       if (s_last) {
         if (threadIdx.x == 0) st<true>(cnt, 0);   // ready for the next launch
         const int nv = min(BR, rows.n - rows.u0);
-        for (int k = threadIdx.x >> 4; k < nv; k += 16) attn_merge_row<BF, D, false, TREE>(p, rq, rows.row(k), rows.head(k));
+        for (int k = threadIdx.x >> 4; k < nv; k += 16) attn_merge_row<BF, D, false>(p, rq, rows.row(k), rows.head(k), op);
       }
       __syncthreads();   // s_last is reused by the next item
     }
@@ -416,7 +428,7 @@ __device__ __forceinline__ void attn_group_items(const AttnArgs& p, int n_reqs, 
 // a third (requests of few rows: the second tile would be padding); else
 // of two (half the reads of the keys and values per row, fewer runs of
 // spans per workgroup).  An attn_rt of 1 or 2 fixes it.
-template <bool BF, int D, bool TREE>
+template <bool BF, int D, int TREE>
 __global__ __launch_bounds__(256) void attn_group_kernel(const AttnArgs p, int n_reqs) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int rt = p.attn_rt;
@@ -439,14 +451,14 @@ __global__ __launch_bounds__(256) void attn_group_kernel(const AttnArgs p, int n
 
 // Slots whose one-tile items outnumber the compute units: one-tile blocks
 // on two workgroups per compute unit, each overlapping the other's waits.
-template <bool BF, int D, bool TREE>
+template <bool BF, int D, int TREE>
 __global__ __launch_bounds__(256, 2) void attn_group2_kernel(const AttnArgs p, int n_reqs) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   attn_group_items<BF, D, 1, TREE, true>(p, n_reqs, smem);
 }
 
 // One wave per (request row, query head), heads of a row adjacent.
-template <bool BF, int D, bool TREE>
+template <bool BF, int D>
 __global__ __launch_bounds__(64) void attn_merge_kernel(const AttnArgs p, int n_reqs) {
   int u = blockIdx.x, r = 0;
   if (n_reqs > 1) r = find_request(p.reqs, n_reqs, u, [&](const ReqDesc& q) { return q.W * p.n_q; });
@@ -454,7 +466,22 @@ __global__ __launch_bounds__(64) void attn_merge_kernel(const AttnArgs p, int n_
   const ReqDesc rq = load_invariant(p.reqs + r);
   if (u >= rq.W * p.n_q) return;
   const int i = u / p.n_q;
-  attn_merge_wave<BF, D, TREE>(p, rq, i, u - i * p.n_q);
+  attn_merge_wave<BF, D>(p, rq, i, u - i * p.n_q);
+}
+
+// The same kernels over one tree's rows from tensors.
+template <bool BF, int D, int RT, bool LOWREG>
+__global__ __launch_bounds__(256, LOWREG ? 2 : 1) void tree_group_kernel(const AttnArgs p, const TreeOp op) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ TreeLds tree;
+  tree_masks_to_lds(op, &tree);
+  __syncthreads();
+  attn_group_items<BF, D, RT, kTreeOp, LOWREG>(p, 1, smem, &op, &tree);
+}
+template <bool BF, int D>
+__global__ __launch_bounds__(64) void tree_merge_kernel(const AttnArgs p, const TreeOp op) {
+  const int i = blockIdx.x / p.n_q;
+  attn_merge_wave<BF, D>(p, tree_req(op), i, blockIdx.x - i * p.n_q, &op);
 }
 
 // Prefill attention of float32 models (bf16: attn_prefill.hip): one workgroup
@@ -545,7 +572,7 @@ __global__ __launch_bounds__(512) void attn_prefill_kernel(const AttnArgs p) {
   }
 }
 
-template <bool BF, int D, bool TREE>
+template <bool BF, int D, int TREE>
 static hipError_t attn_dispatch(const AttnArgs& a, int n_reqs, int max_blocks, bool prefill, hipStream_t s) {
   if (max_blocks > kMaxBlocks || n_reqs < 1) return hipErrorInvalidValue;
   if (prefill) {
@@ -561,6 +588,7 @@ static hipError_t attn_dispatch(const AttnArgs& a, int n_reqs, int max_blocks, b
   const long long rows = (long long)hpg * (a.M - n_reqs + 1);
   const long long items = (long long)n_reqs * a.n_kv * ((rows + 15) / 16) * ((max_blocks + kAttnSpan - 1) / kAttnSpan);
   const int cus = a.cus > 0 ? std::min(a.cus, kAttnGrid) : kAttnGrid;
+  if (BF && TREE && a.wave_tiles) return launch_tree_pass(a, n_reqs, cus, s);
   if (BF && a.wave_tiles) {
     const hipError_t e = launch_attn_spans(a, n_reqs, 2 * cus, s);
     if (e != hipSuccess) return e;
@@ -573,8 +601,38 @@ static hipError_t attn_dispatch(const AttnArgs& a, int n_reqs, int max_blocks, b
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.merge_last) return e;
-  attn_merge_kernel<BF, D, TREE><<<a.M * a.n_q, 64, 0, s>>>(a, n_reqs);
+  attn_merge_kernel<BF, D><<<a.M * a.n_q, 64, 0, s>>>(a, n_reqs);
   return hipGetLastError();
+}
+
+template <bool BF, int D>
+static hipError_t tree_dispatch(const AttnArgs& a, const TreeOp& op, int blocks, hipStream_t s) {
+  const int rows = a.n_q / a.n_kv * op.W, spans = (blocks + kAttnSpan - 1) / kAttnSpan;
+  const long long items = (long long)a.n_kv * ((rows + 15) / 16) * spans;
+  const long long items2 = (long long)a.n_kv * ((rows + 31) / 32) * spans;
+  const int cus = a.cus > 0 ? std::min(a.cus, kAttnGrid) : kAttnGrid;
+  if (BF && a.wave_tiles) return launch_tree_op(a, op, cus, s);
+  // the block sizes and kernels of attn_dispatch
+  if (items > cus && a.attn_rt == 0) {
+    tree_group_kernel<BF, D, 1, true><<<(int)std::min<long long>(2 * cus, (items + 7) / 8 * 8), 256,
+                                       attn_span_lds_bytes<BF, D, 1>(), s>>>(a, op);
+  } else {
+    const int grid = (int)std::min<long long>(cus, (items + 7) / 8 * 8);
+    const int rt = a.attn_rt == 1 || a.attn_rt == 2 ? a.attn_rt : items <= grid || 2 * items < 3 * items2 ? 1 : 2;
+    if (rt == 1) tree_group_kernel<BF, D, 1, false><<<grid, 256, attn_span_lds_bytes<BF, D, 1>(), s>>>(a, op);
+    else tree_group_kernel<BF, D, 2, false><<<grid, 256, attn_span_lds_bytes<BF, D, 2>(), s>>>(a, op);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.merge_last) return e;
+  tree_merge_kernel<BF, D><<<op.W * a.n_q, 64, 0, s>>>(a, op);
+  return hipGetLastError();
+}
+
+hipError_t launch_tree_attention(bool bf16, const AttnArgs& a, const TreeOp& op, int blocks, hipStream_t s) {
+  if (op.W < 1 || op.W > 32 || blocks < 1 || blocks > kMaxBlocks) return hipErrorInvalidValue;
+  if (a.head_dim == 128) return bf16 ? tree_dispatch<true, 128>(a, op, blocks, s) : tree_dispatch<false, 128>(a, op, blocks, s);
+  if (a.head_dim == 64) return bf16 ? tree_dispatch<true, 64>(a, op, blocks, s) : tree_dispatch<false, 64>(a, op, blocks, s);
+  return hipErrorInvalidValue;
 }
 
 // Kernels whose dynamic LDS may exceed the default 64 KiB limit.
@@ -615,9 +673,11 @@ static hipError_t prepare_staged() {
 template <bool BF, int D>
 static hipError_t prepare_attention() {
   auto allow = [](const void* k, int bytes) { return hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-  hipError_t e = allow(reinterpret_cast<const void*>(&attn_group_kernel<BF, D, false>), attn_span_lds_bytes<BF, D, 2>());
+  hipError_t e = allow(reinterpret_cast<const void*>(&attn_group_kernel<BF, D, kChain>), attn_span_lds_bytes<BF, D, 2>());
   if (e == hipSuccess)
-    e = allow(reinterpret_cast<const void*>(&attn_group_kernel<BF, D, true>), attn_span_lds_bytes<BF, D, 2>());
+    e = allow(reinterpret_cast<const void*>(&attn_group_kernel<BF, D, kTree>), attn_span_lds_bytes<BF, D, 2>());
+  if (e == hipSuccess)
+    e = allow(reinterpret_cast<const void*>(&tree_group_kernel<BF, D, 2, false>), attn_span_lds_bytes<BF, D, 2>());
   if constexpr (!BF)
     if (e == hipSuccess)
       e = allow(reinterpret_cast<const void*>(&attn_prefill_kernel<D>), attn_prefill_lds_bytes<D>());
@@ -640,14 +700,15 @@ hipError_t prepare_kernels() {
 #undef AS2D_P
   if (e == hipSuccess) e = prepare_wide();
   if (e == hipSuccess) e = prepare_attn_prefill();
+  if (e == hipSuccess) e = prepare_tree();
   return e;
 }
 
 hipError_t launch_attention(bool bf16, const AttnArgs& a, int n_reqs, int max_blocks, bool prefill, hipStream_t s) {
 #define AS2D_A(bf, dim, tr) \
-  if (bf16 == bf && a.head_dim == dim && (a.tree != 0) == tr) return attn_dispatch<bf, dim, tr>(a, n_reqs, max_blocks, prefill, s);
-  AS2D_A(true, 128, false) AS2D_A(true, 64, false) AS2D_A(false, 128, false) AS2D_A(false, 64, false)
-  AS2D_A(true, 128, true) AS2D_A(true, 64, true) AS2D_A(false, 128, true) AS2D_A(false, 64, true)
+  if (bf16 == bf && a.head_dim == dim && (a.tree ? kTree : kChain) == tr) return attn_dispatch<bf, dim, tr>(a, n_reqs, max_blocks, prefill, s);
+  AS2D_A(true, 128, kChain) AS2D_A(true, 64, kChain) AS2D_A(false, 128, kChain) AS2D_A(false, 64, kChain)
+  AS2D_A(true, 128, kTree) AS2D_A(true, 64, kTree) AS2D_A(false, 128, kTree) AS2D_A(false, 64, kTree)
 #undef AS2D_A
   return hipErrorInvalidValue;
 }

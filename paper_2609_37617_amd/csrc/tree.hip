@@ -1,6 +1,6 @@
-// Passes over trees of candidates: rows from device tensors into a cache
-// layer, greedy verification along a tree, and the accepted path's cache
-// rows moved together.
+// Passes over trees of candidates: greedy verification along a tree and the
+// accepted path's cache rows moved together; rows from device tensors into a
+// cache layer.
 //
 // Row i of a request sits in cache row L0 + i and sees the committed keys and
 // the rows in its mask (attn.h); its rotary position is L0 and its depth.
@@ -12,10 +12,7 @@ namespace as2d {
 
 // ---------------------------------------------------------------------------
 // Keys and values [n][n_kv][D] of any strides into cache rows pos0 .. of a
-// layer (layout: kernels.h), and for a tree attention its queries as
-// float32 rows and the descriptors of its rows and its request.  One
-// workgroup per row; the smallest part of such a call (32 rows of the 7B
-// shape read and write 0.6 MB).
+// layer (layout: kernels.h), one workgroup per row.
 
 template <bool SRC16> __device__ __forceinline__ float src_value(const void* p, long long i) {
   if constexpr (SRC16) return bf2f(ldg(static_cast<const uint16_t*>(p) + i));
@@ -45,23 +42,10 @@ __global__ __launch_bounds__(256) void put_rows_kernel(const PutRows a) {
       *gmem(vb + v_elem(pos, 0, dd, D, false)) = v;
     }
   }
-  if (!a.q_out) return;
-  for (int i = threadIdx.x; i < a.n_q * D; i += 256) {
-    const int h = i / D, dd = i - h * D;
-    *gmem(a.q_out + (size_t)r * a.n_q * D + i) = src_value<SRC16>(a.q.data, r * a.q.row_stride + h * a.q.head_stride + dd);
-  }
-  if (threadIdx.x == 0) {
-    RowDesc rd{};
-    rd.pos = pos;
-    rd.slot = a.slot;
-    rd.mask = a.mask[r & 31];
-    a.rows[r] = rd;
-    if (r == 0) *a.req = ReqDesc{0, (int)gridDim.x, a.pos0, a.slot};
-  }
 }
 
 hipError_t launch_put_rows(bool bf16, bool src_bf16, const PutRows& a, int n, hipStream_t s) {
-  if (n < 1 || (a.q_out && n > 32)) return hipErrorInvalidValue;
+  if (n < 1) return hipErrorInvalidValue;
   if (bf16 && src_bf16) put_rows_kernel<true, true><<<n, 256, 0, s>>>(a);
   else if (bf16) put_rows_kernel<true, false><<<n, 256, 0, s>>>(a);
   else if (src_bf16) put_rows_kernel<false, true><<<n, 256, 0, s>>>(a);

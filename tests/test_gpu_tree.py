@@ -118,6 +118,39 @@ def test_attention_with_large_scores_and_values(served):
     assert (got.float() - want).abs().max() <= 4.0 * (2.0 ** -8 if shape.dtype != as2d.F32 else 2.0 ** -22)
 
 
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_non_finite_rows_reach_only_the_rows_that_see_them(served, what, value):
+    shape, m = served
+    parents = [-1, -1, 0, 1, 1, 3]
+    for keys in (126, 2500):
+        q, k, v, K, V = tensors(shape, 7, keys, 8)
+        m.prefill(0, np.zeros(0, np.uint16), np.zeros(keys, np.int32))
+        m.write_kv(0, 1, K, V)
+        clean = m.tree_attention(0, 1, q, k, v, parents)
+        (k if what == "k" else v)[2, :, 3] = value    # candidate 1, which candidates 3, 4 and 5 follow
+        got = m.tree_attention(0, 1, q, k, v, parents)
+        sees = trees.visible(parents)[:, 2]
+        assert torch.equal(got[~sees], clean[~sees])
+        if what == "v" or value != value:
+            assert torch.isnan(got[sees]).any(-1).all()
+
+
+LONG = [QWEN05B, QWEN7B]
+
+
+@pytest.mark.parametrize("keys,rows,branch", [(8000, 32, 3), (7937, 31, 1), (8063, 9, 2), (5000, 32, 31), (8128, 18, 2)])
+@pytest.mark.parametrize("shape", LONG, ids=lambda s: s.name)
+def test_attention_over_long_caches(shape, keys, rows, branch):
+    m = heads_model(shape, 8192, max_requests=1)
+    attend_and_check(m, shape, keys, rows, heap(rows - 1, branch), keys + rows)
+    m.set_cu_budget(64)   # longer runs, the last ones ragged
+    attend_and_check(m, shape, keys, rows, heap(rows - 1, branch), keys + rows)
+    m.set_cu_budget(1)    # one run holds every key
+    attend_and_check(m, shape, 2100, rows, heap(rows - 1, branch), keys + rows)
+    m.close()
+
+
 def test_attention_of_other_strides(served):
     """Heads before rows, rows further apart, an output inside a larger tensor."""
     shape, m = served
@@ -336,6 +369,46 @@ def test_every_branch_is_its_own_chain(model):
         prefilled(m, shape, 0, 123)
         m.verify(0, [cands[i - 1] for i in rows[1:]])
         assert close(got[rows], m.logits(0), shape), leaf
+
+
+def test_passes_over_long_caches():
+    """Trees at 7B heads over slots of more than 2,048 positions, one request and
+    two: every branch is its own chain's to rounding; a call of chains alone
+    has as2d_verify_batch's bits."""
+    from dataclasses import replace
+    shape = replace(TINY_BF16, name="long", n_q_heads=28, n_kv_heads=4, head_dim=128, n_layers=1)
+    _, m = make_pair(shape, max_requests=2, max_kv_len=4096, max_k=31, oracle=False)
+    m.set_keep_logits(True)
+    rng = np.random.default_rng(6)
+    k = 31
+    parents = [[int(rng.integers(-1, i)) for i in range(k)] for _ in range(2)]
+    cands = [rng.integers(0, shape.vocab, k).tolist() for _ in range(2)]
+
+    def start():
+        for r in range(2):
+            m.prefill(r, np.zeros(0, np.uint16), np.arange(3000 + 700 * r, dtype=np.int32) % shape.vocab)
+    start()
+    m.verify_tree(0, cands[0], parents[0])
+    alone = m.logits(0)
+    start()
+    m.verify_tree_batch([0, 1], cands, parents)
+    both = [m.logits(0), m.logits(1)]
+    assert close(alone, both[0], shape)
+    for r in range(2):
+        sees = trees.visible(parents[r])
+        for leaf in [i for i in range(k) if i not in parents[r]][:8]:
+            rows = np.flatnonzero(sees[leaf + 1])
+            start()
+            m.verify(r, [cands[r][i - 1] for i in rows[1:]])
+            assert close(both[r][rows], m.logits(r), shape), (r, leaf)
+    start()
+    a = m.verify_batch([0, 1], cands)
+    la = [m.logits(0), m.logits(1)]
+    start()
+    b = m.verify_tree_batch([0, 1], cands)
+    assert [dict(x, path=list(range(x["accepted_len"]))) for x in a] == b
+    assert all(np.array_equal(x, m.logits(r)) for r, x in enumerate(la))
+    m.close()
 
 
 def test_no_child_is_accepted(model):
