@@ -21,9 +21,9 @@
 //
 // Rounding.  Exponentials are float32 (2^x by the hardware, about 1 unit in
 // the last place, with the argument's rounding put back: x is formed in 64
-// bits, 2^x = 2^float(x) (1 + (x - float(x)) ln 2)); everything summed,
-// compared or logged is 64 bits, so that a random number next to a border
-// falls on the same side as in exact arithmetic.
+// bits, 2^x = 2^float(x) (1 + (x - float(x)) ln 2)); what is summed over a row, compared or logged is 64
+// bits, so that a random number next to a border falls on the same side as in
+// exact arithmetic.
 #include "common.h"
 
 namespace as2d {
@@ -128,7 +128,8 @@ template <bool BF> __device__ __forceinline__ void load_chunk(const void* base, 
   }
 }
 
-// 2^(x c - top).
+// 2^(x c - top).  (x c - top as a pair of float32 instead of 64 bits: one pass
+// over 16 x 13 rows of 152,064 logits 28.3 us against 24.8.)
 __device__ __forceinline__ float power(float x, double c, double top) {
   const double y = fmax(__builtin_fma((double)x, c, -top), -200.0);   // 2^-200 and less (x = -inf) are 0 in float32
   const float f = (float)y;
@@ -210,7 +211,11 @@ struct RowStat {
   double sum, top;
   int bad;
 };
-__device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks) {
+template <bool COH> __device__ __forceinline__ SamplePart load_part(const SamplePart* p) {
+  if constexpr (COH) return SamplePart{ld_coherent(&p->sum), ld_coherent(&p->top)};
+  else return *p;
+}
+template <bool COH> __device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks) {
   const int lane = threadIdx.x & 63;
   constexpr int B = 4;   // a lane's first parts, kept (262,144 tokens: all of them)
   SamplePart p[B];
@@ -219,7 +224,7 @@ __device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks) 
 #pragma unroll
   for (int i = 0; i < B; ++i) {
     p[i] = SamplePart{0.0, -INFINITY};
-    if (64 * i + lane < chunks) p[i] = part[64 * i + lane];
+    if (64 * i + lane < chunks) p[i] = load_part<COH>(part + 64 * i + lane);
   }
 #pragma unroll
   for (int i = 0; i < B; ++i) {
@@ -227,16 +232,19 @@ __device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks) 
     top = fmax(top, p[i].top);
   }
   for (int i = 64 * B + lane; i < chunks; i += 64) {
-    bad |= part[i].top != part[i].top;
-    top = fmax(top, part[i].top);
+    const double t = load_part<COH>(part + i).top;
+    bad |= t != t;
+    top = fmax(top, t);
   }
   top = wave_max64(top);
   double s = 0.0;
 #pragma unroll
   for (int i = 0; i < B; ++i)
     if (p[i].top > -INFINITY) s += rescale(p[i].sum, p[i].top, top);
-  for (int i = 64 * B + lane; i < chunks; i += 64)
-    if (part[i].top > -INFINITY) s += rescale(part[i].sum, part[i].top, top);
+  for (int i = 64 * B + lane; i < chunks; i += 64) {
+    const SamplePart v = load_part<COH>(part + i);
+    if (v.top > -INFINITY) s += rescale(v.sum, v.top, top);
+  }
   return RowStat{wave_sum64(s), top, __ballot(bad) != 0 || !(top > -INFINITY)};
 }
 __device__ __forceinline__ double prob(float x, const RowStat& t, double c) {
@@ -249,20 +257,10 @@ __device__ __forceinline__ float log_prob(float x, double top, double log_sum, d
 
 // ---- kernels ----------------------------------------------------------------
 
-// Maximum and sum of every chunk of the target's rows and of the drafter's
-// rows with children, a chunk per wave.  The one pass over the logits that
-// cannot be avoided.
-template <bool BF>
-__global__ __launch_bounds__(kBlock) void sample_stats_kernel(const SampleArgs a) {
-  const int chunk = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6), row = blockIdx.y;
-  const int which = (int)blockIdx.z >= a.n, r = blockIdx.z - which * a.n;
-  const Req q = load_req(a, r);
-  if (!q.ok || row > q.k || chunk >= a.chunks) return;
-  if (which && (q.drow0 < 0 || !children_of(lane_parent(a, q), row))) return;
+// A wave's chunk of a row: its sum and the top it is scaled by.
+template <bool BF> __device__ __forceinline__ SamplePart chunk_part(const void* base, long long row, int chunk, int vocab, double c) {
   float x[kPer];
-  load_chunk<BF>(which ? a.draft : a.target, (which ? q.drow0 + row : q.row0 + row) * (which ? a.d_stride : a.t_stride), chunk,
-                 a.vocab, x);
-  const double c = which ? q.dc : q.c;
+  load_chunk<BF>(base, row, chunk, vocab, x);
   float m = -INFINITY;
   bool bad = false;
 #pragma unroll
@@ -279,7 +277,23 @@ __global__ __launch_bounds__(kBlock) void sample_stats_kernel(const SampleArgs a
       s += (double)((power(x[e], c, top) + power(x[e + 1], c, top)) + (power(x[e + 2], c, top) + power(x[e + 3], c, top)));
     s = wave_sum64(s);
   }
-  if ((threadIdx.x & 63) == 0) part_of(a, r, which, row)[chunk] = SamplePart{s, top};
+  return SamplePart{s, top};
+}
+
+// The parts of every chunk of the target's rows and of the drafter's rows with
+// children, a chunk per wave.  The one pass over the logits that cannot be
+// avoided.
+template <bool BF>
+__global__ __launch_bounds__(kBlock) void sample_stats_kernel(const SampleArgs a) {
+  const int chunk = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6), row = blockIdx.y;
+  const int which = (int)blockIdx.z >= a.n, r = blockIdx.z - which * a.n;
+  const Req q = load_req(a, r);
+  if (!q.ok || row > q.k || chunk >= a.chunks) return;
+  if (which && (q.drow0 < 0 || !children_of(lane_parent(a, q), row))) return;
+  const SamplePart p =
+      chunk_part<BF>(which ? a.draft : a.target, (which ? q.drow0 + row : q.row0 + row) * (which ? a.d_stride : a.t_stride),
+                     chunk, a.vocab, which ? q.dc : q.c);
+  if ((threadIdx.x & 63) == 0) part_of(a, r, which, row)[chunk] = p;
 }
 
 // Sum of max(p - C q, 0) over a wave's chunk; ps, qs: 1 / sum and C / sum.
@@ -306,7 +320,7 @@ __global__ __launch_bounds__(kWide) void sample_stage_kernel(const SampleArgs a,
   const Req q = load_req(a, r);
   if (!q.ok || row > q.k || q.drow0 < 0 || __popc(children_of(lane_parent(a, q), row)) <= s) return;
   if (wave < 2) {
-    const RowStat t = row_stat(part_of(a, r, wave, row), a.chunks);
+    const RowStat t = row_stat<false>(part_of(a, r, wave, row), a.chunks);
     if (lane == 0) s_stat[wave] = t;
   } else if (wave == 2) {
     double cut = 1.0;
@@ -371,12 +385,12 @@ template <class Goal> __device__ __forceinline__ int find_in_run(double v, Goal&
 
 // The walk and the token.  Every test's outcome follows from its node's
 // earlier siblings having failed, so all are made at once, a candidate per
-// lane, and the walk follows bits.  `gridDim.x` workgroups per request: more
+// lane, and the walk follows bits.  `blocks` workgroups per request: more
 // than one where a drafter's distribution may have to be taken off the
 // node's; each then makes the same walk, sums its share of what is left, and
-// the last to finish draws the token.
-template <bool BF>
-__global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a) {
+// the last to finish draws the token.  FUSED: one workgroup, in the kernel that
+// made the parts.
+template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(const SampleArgs& a, const Req& q, int block, int blocks) {
   constexpr int kWavesW = kWide / 64;
   __shared__ RowStat s_stat[2][32];
   __shared__ double s_left[32], s_again[32], s_log[32];
@@ -384,9 +398,8 @@ __global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a
   __shared__ int s_cand[32], s_bad, s_at, s_n, s_path[32], s_last;
   __shared__ double s_cut, s_cutoff[32];
   __shared__ Find s_find;
-  const int r = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const bool writes = blockIdx.x == 0;
-  const Req q = load_req(a, r);
+  const int r = q.r, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const bool writes = block == 0;
   const bool drafted = q.drow0 >= 0;
   if (tid == 0) s_bad = !q.ok || (a.gate && a.gate[r].nan_flag);
   const int parent = lane_parent(a, q);
@@ -409,7 +422,7 @@ __global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a
     const uint32_t children = children_of(parent, row);
     if (!which && lane == 0) s_children[row] = children;
     if (which && (!drafted || !children)) continue;
-    const RowStat st = row_stat(part_of(a, r, which, row), a.chunks);
+    const RowStat st = row_stat<FUSED>(part_of(a, r, which, row), a.chunks);
     if (lane == 0) {
       s_stat[which][row] = st;
       if (st.bad) s_bad = 1;
@@ -495,15 +508,15 @@ __global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a
     d = s_stat[1][at];
     qs = taken / d.sum;
     double* out = a.left + (size_t)r * a.chunks;
-    for (int chunk = blockIdx.x * kWavesW + wave; chunk < a.chunks; chunk += gridDim.x * kWavesW) {
+    for (int chunk = block * kWavesW + wave; chunk < a.chunks; chunk += blocks * kWavesW) {
       const double v = chunk_left<BF>(a, trow, drow, chunk, t.top, q.c, ps, d.top, q.dc, qs);
       if (lane == 0) st<true>(out + chunk, v);
     }
-    if (gridDim.x > 1) {
+    if (blocks > 1) {
       wait_vmem();
       __syncthreads();
       if (tid == 0) {
-        s_last = counter_add(a.ticket + r, 1) == (int)gridDim.x - 1;
+        s_last = counter_add(a.ticket + r, 1) == blocks - 1;
         if (s_last) st<true>(a.ticket + r, 0);   // ready for the next call
       }
       __syncthreads();
@@ -555,11 +568,12 @@ __global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a
           if (ch >= 0) {
             float y[kPer];
             load_chunk<BF>(a.target, trow, ch, a.vocab, y);
-            const double top = part[ch].top;
-            if (top > -INFINITY)
+            const double top = load_part<FUSED>(part + ch).top;
+            if (top > -INFINITY) {
 #pragma unroll
               for (int e = 0; e < kPer; ++e)
                 v += is_gone(ch * kSampleChunk + column<BF>(e)) ? 0.0 : (double)power(y[e], q.c, top);
+            }
             v = wave_sum64(v);
           }
           if (lane == 0) s_again[i] = v;
@@ -567,7 +581,7 @@ __global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a
       __syncthreads();
       const auto left = [&](int i) -> double {
         if (taken > 0.0) return ld_coherent(a.left + (size_t)r * a.chunks + i);
-        const SamplePart p = part[i];
+        const SamplePart p = load_part<FUSED>(part + i);
         double v = p.sum;
         for (uint32_t b = gone; b; b &= b - 1)
           if (chunk_of(__builtin_ctz(b)) == i) v = s_again[__builtin_ctz(b)];
@@ -609,7 +623,7 @@ __global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a
       if (taken > 0.0) {
         v = left_of(power(y, q.c, t.top), ps, power(logit<BF>(a.draft, drow + col), q.dc, d.top), qs);
       } else {
-        const double top = part[chunk].top;
+        const double top = load_part<FUSED>(part + chunk).top;
         if (top > -INFINITY && !is_gone(col)) v = rescale((double)power(y, q.c, top), top, t.top);
       }
     }
@@ -618,9 +632,53 @@ __global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a
   }
 }
 
+template <bool BF> __global__ __launch_bounds__(kWide) void sample_finish_kernel(const SampleArgs a) {
+  sample_finish<BF, false>(a, load_req(a, blockIdx.y), blockIdx.x, gridDim.x);
+}
+
+// Both in one launch, without a drafter's rows: the last workgroup of a request
+// to have made its parts finishes it.
+template <bool BF> __global__ __launch_bounds__(kWide) void sample_fused_kernel(const SampleArgs a) {
+  __shared__ int s_last;
+  const int row = blockIdx.y, r = blockIdx.z, chunk = blockIdx.x * (kWide / 64) + (threadIdx.x >> 6);
+  const Req q = load_req(a, r);
+  if (row > q.k) return;
+  if (q.ok) {
+    if (chunk < a.chunks) {
+      const SamplePart p = chunk_part<BF>(a.target, (q.row0 + row) * a.t_stride, chunk, a.vocab, q.c);
+      if ((threadIdx.x & 63) == 0) {
+        SamplePart* out = part_of(a, r, 0, row) + chunk;
+        st<true>(&out->sum, p.sum);
+        st<true>(&out->top, p.top);
+      }
+    }
+    wait_vmem();
+    __syncthreads();   // the workgroup's parts are stored
+    if (threadIdx.x == 0) {
+      s_last = counter_add(a.ticket + r, 1) == (int)gridDim.x * (q.k + 1) - 1;
+      if (s_last) st<true>(a.ticket + r, 0);   // ready for the next call
+    }
+    __syncthreads();
+    if (!s_last) return;
+  } else if (blockIdx.x) {
+    return;   // refused: nothing to wait for
+  }
+  sample_finish<BF, true>(a, q, 0, 1);
+}
+
+// Up to this many workgroups (one per compute unit) a call without a drafter is
+// one launch: 16 requests of one row of 152,064 logits (160 workgroups) 12.5 us
+// against 15.3 in two, 1 request of 32 rows (320) 21.7 against 18.9: past one
+// workgroup a unit the larger kernel's fewer waves hold the pass back.
+constexpr long long kFusedBlocks = 256;
+
 template <bool BF> hipError_t run(const SampleArgs& a, bool draft, hipStream_t s) {
   static_assert(kSampleChunk == kWide, "the token's chunk: a column per thread");
   const auto blocks = [&](int threads) { return (a.chunks + threads / 64 - 1) / (threads / 64); };
+  if (!draft && (long long)blocks(kWide) * (a.k + 1) * a.n <= kFusedBlocks) {
+    sample_fused_kernel<BF><<<dim3(blocks(kWide), a.k + 1, a.n), kWide, 0, s>>>(a);
+    return hipGetLastError();
+  }
   sample_stats_kernel<BF><<<dim3(blocks(kBlock), a.k + 1, (draft ? 2 : 1) * a.n), kBlock, 0, s>>>(a);
   if (draft)
     for (int st = 1; st < a.max_children; ++st)
