@@ -450,6 +450,25 @@ bool wave_tiles(const as2d_ctx* c, int M, const ReqDesc* reqs, int n, int part_s
   return items > 2 * (c->grid_cus > 0 ? std::min(c->grid_cus, kAttnGrid) : kAttnGrid);
 }
 
+// Whether the attention of rows in trees takes runs of keys per workgroup
+// (attn_tree.hip) instead of 128 keys and 16 rows (attn_group_items): past as
+// many (span, KV head, row tile) items as the latter has workgroups, where one
+// launch does not join the states anyway.  A call of as2d_tree_attention,
+// groups against runs: 7B heads, 1 row over 8,000 keys (252 items) 17.6 us
+// against 18.6, over 16,000 (500) 25.0 against 23.6; 9 rows over 4,000 (512)
+// 18.0 against 18.3, over 8,000 (1,008) 26.0 against 21.3; 17 rows over 2,100
+// (544) 23.6 against 22.4; 3B heads, 17 rows over 2,100 (306) 18.1 against
+// 22.0, over 4,000 (576) 23.6 against 21.6; 0.5B heads, 32 rows over 2,100 (476)
+// 16.9 against 18.3, over 4,000 (896) 20.8 against 18.4.
+bool tree_by_runs(const as2d_ctx* c, const ReqDesc* reqs, int n, int part_spans) {
+  if (!c->bf16 || c->attn_rt || merge_last(part_spans)) return false;
+  const int hpg = c->cfg.n_q_heads / c->cfg.n_kv_heads;
+  long long items = 0;
+  for (int r = 0; r < n; ++r)
+    items += (long long)c->cfg.n_kv_heads * ((hpg * reqs[r].W + 15) / 16) * ((reqs[r].L0 + reqs[r].W - 1) / kAttnSpanKeys + 1);
+  return items > 2 * (c->grid_cus > 0 ? std::min(c->grid_cus, kAttnGrid) : kAttnGrid);
+}
+
 // Kernel launches of one forward pass over the rows and requests in the
 // device descriptors: n_att attention requests (d_reqs[0..n_att)), n_fin
 // finish requests (d_reqs[max_requests..)) covering fin_rows rows;
@@ -805,7 +824,9 @@ int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool v
     HIP_TRY(c, hipMemcpyAsync(c->b.d_rows, c->h_rows, sizeof(RowDesc) * M, hipMemcpyHostToDevice, s));
     HIP_TRY(c, hipMemcpyAsync(c->b.d_reqs, c->h_reqs, sizeof(ReqDesc) * 2 * mr, hipMemcpyHostToDevice, s));
   }
-  const bool tiles = verify_call && !persistent && wave_tiles(c, M, c->h_reqs, n_att, c->b.part_spans);
+  const bool tiles = verify_call && !persistent &&
+                     (tree == kPassTrees ? tree_by_runs(c, c->h_reqs, n_att, c->b.part_spans)
+                                         : wave_tiles(c, M, c->h_reqs, n_att, c->b.part_spans));
   if (graph) {
     hipGraphExec_t ex = nullptr;
     int rc = graph_for(c, M, n_att, n_fin, fin_rows, persistent, tiles, tree, &ex);
@@ -1765,7 +1786,7 @@ int as2d_tree_attention(as2d_ctx* c, int32_t req, int32_t layer, int32_t n_rows,
   t.merge_last = merge_last(spans);
   t.attn_cnt = c->b.attn_cnt;
   t.M = n_rows;
-  t.wave_tiles = wave_tiles(c, n_rows, &rq, 1, spans);
+  t.wave_tiles = tree_by_runs(c, &rq, 1, spans);
   t.attn_rt = c->attn_rt;
   t.cus = c->grid_cus;
   HIP_TRY(c, launch_tree_attention(c->bf16, t, op, blocks, s));

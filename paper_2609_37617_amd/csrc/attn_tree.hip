@@ -32,16 +32,15 @@ constexpr float kTreeSlack = 8.0f;                             // 2^8 over the m
 template <int D> __host__ __device__ constexpr int tree_units() { return kTreeStep * D * 4 / 16; }   // of a step's keys, or values
 template <int D> __host__ __device__ constexpr int tree_lds_bytes() { return 2 * 2 * tree_units<D>() * 16; }
 
-// Spans per run and items of a launch of G workgroups, T tiles a wave.
-template <class Reqs>
-__device__ __forceinline__ void tree_runs(const AttnArgs& p, const Reqs& reqs, int n_reqs, int G, int T, int& R, int& total) {
-  const int hpg = p.n_q / p.n_kv;
-  const auto spans = [](const ReqDesc& rq) { return (rq.L0 + rq.W - 1) / kAttnSpanKeys + 1; };
-  const auto groups = [=](const ReqDesc& rq) { return p.n_kv * ((hpg * rq.W + 64 * T - 1) / (64 * T)); };
-  const auto items = [=](const ReqDesc& rq, int r) { return groups(rq) * ((spans(rq) + r - 1) / r); };
-  if constexpr (std::is_same_v<Reqs, ReqDesc>) run_length_of(reqs, G, items, groups, R, total);
-  else attn_run_length(reqs, n_reqs, G, items, groups, R, total);
-}
+// Spans per run and items of a launch of G workgroups with T tiles a wave: of a
+// pass's requests (device), or of one (host).
+__host__ __device__ inline int tree_spans(const ReqDesc& rq) { return (rq.L0 + rq.W - 1) / kAttnSpanKeys + 1; }
+struct TreeItems {
+  int n_kv, hpg, rows;   // rows of a workgroup
+  __host__ __device__ int per(const ReqDesc& rq) const { return (hpg * rq.W + rows - 1) / rows; }
+  __host__ __device__ int operator()(const ReqDesc& rq) const { return n_kv * per(rq); }
+  __host__ __device__ int operator()(const ReqDesc& rq, int r) const { return n_kv * per(rq) * ((tree_spans(rq) + r - 1) / r); }
+};
 
 // One item: spans [sp0, sp1) of rq for rows u0 .. of KV head g.
 template <int D, int T, bool OP>
@@ -55,9 +54,6 @@ __device__ __forceinline__ void tree_run(const AttnArgs& p, const TreeOp* op, Tr
   const uint4* kb = reinterpret_cast<const uint4*>(p.k_cache + head);
   const uint4* vb = reinterpret_cast<const uint4*>(p.v_cache + head);
   u32x4* L = reinterpret_cast<u32x4*>(smem);   // keys [2][U], values [2][U]
-  if constexpr (OP)
-    if (sp1 * kAttnSpanKeys > rq.L0) tree_put<true, D, kTreeThreads>(p, *op, g, tree);
-
   // Keys: unit u (16 bytes) of key k at u ^ (k % 16), so that the 16 keys a
   // fragment read takes at one u lie in 16 different bank groups.  Values:
   // fragment order (block of 16 dimensions and one part, lane).
@@ -88,27 +84,26 @@ __device__ __forceinline__ void tree_run(const AttnArgs& p, const TreeOp* op, Tr
     }
   };
   const int s0 = sp0 * kTreeStepsPerSpan, s1 = min(sp1 * kTreeStepsPerSpan, last / kTreeStep + 1);
+  // (the first step's reads ahead of this, where they do not take the rows: 64
+  // us instead of 56 over 32,704 keys, the loop's waits change with it)
+  if constexpr (OP)
+    if (sp1 * kAttnSpanKeys > rq.L0) tree_put<true, D, kTreeThreads>(p, *op, g, tree);
   request(s0);
 
   // this lane's rows, one per tile; rows past the group's repeat the last one
   const bool active = rows.u0 + 16 * T * rp < rows.n;
-  int row[T], h[T];
-  uint32_t mask[T];
+  const auto row_of = [&](int t) { return 16 * (T * rp + t) + lr; };
   Op2 q[T][KS];
 #pragma unroll
   for (int t = 0; t < T; ++t) {
-    const int rr = 16 * (T * rp + t) + lr;
-    row[t] = rows.row(rr);
-    h[t] = rows.head(rr);
+    const int row = rows.row(row_of(t)), h = rows.head(row_of(t));
     if constexpr (OP) {
-      mask[t] = tree->mask[row[t]];
       typedef uint16_t run __attribute__((ext_vector_type(8), aligned(2)));
-      const uint16_t* src = static_cast<const uint16_t*>(op->q.data) + row[t] * op->q.row_stride + h[t] * op->q.head_stride + 8 * lg;
+      const uint16_t* src = static_cast<const uint16_t*>(op->q.data) + row * op->q.row_stride + h * op->q.head_stride + 8 * lg;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) q[t][ks].h = __builtin_bit_cast(uint4, *gmem(reinterpret_cast<const run*>(src + 32 * ks)));
     } else {
-      mask[t] = ldg(&p.rows[rq.row_start + row[t]].mask);
-      const float4* src = reinterpret_cast<const float4*>(p.q + (size_t)(rq.row_start + row[t]) * p.n_q * D + h[t] * D + 8 * lg);
+      const float4* src = reinterpret_cast<const float4*>(p.q + (size_t)(rq.row_start + row) * p.n_q * D + h * D + 8 * lg);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const float4 v[2] = {ldg(src + 8 * ks), ldg(src + 8 * ks + 1)};
@@ -128,7 +123,7 @@ __device__ __forceinline__ void tree_run(const AttnArgs& p, const TreeOp* op, Tr
 
   auto chunk = [&](int step) {
     const int buf = step & 1, kc = step * kTreeStep + kh * kAttnChunk;
-    if (kc > last || !active) return;
+    if (!active || kc > last) return;
     f4 sa[T][2];
 #pragma unroll
     for (int t = 0; t < T; ++t) sa[t][0] = sa[t][1] = f4{0.f, 0.f, 0.f, 0.f};
@@ -155,11 +150,16 @@ __device__ __forceinline__ void tree_run(const AttnArgs& p, const TreeOp* op, Tr
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[kt][i] = sa[t][kt][i] * p.scale;
       if (kc + kAttnChunk > rq.L0) {   // the tree's rows
+        asm volatile("");              // a branch: the other chunks do without the masks
+        const int row = rows.row(row_of(t));
+        const uint32_t mask = OP ? tree->mask[row] : ldg(&p.rows[rq.row_start + row].mask);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!tree_sees(mask[t], kc + 16 * kt + 4 * lg + i, rq.L0, rq.L0 + row[t])) s[kt][i] = -INFINITY;
+            if (!tree_sees(mask, kc + 16 * kt + 4 * lg + i, rq.L0, rq.L0 + row)) s[kt][i] = -INFINITY;
+        if constexpr (OP)
+          if (mask & tree->bad) S[t] = NAN;
       }
       float mx = s[0][0];
 #pragma unroll
@@ -183,8 +183,6 @@ __device__ __forceinline__ void tree_run(const AttnArgs& p, const TreeOp* op, Tr
 #pragma unroll
         for (int i = 0; i < 4; ++i) pj[kt][i] = exp2_hw(s[kt][i] - ref);
       S[t] += (((pj[0][0] + pj[0][1]) + pj[0][2]) + pj[0][3]) + (((pj[1][0] + pj[1][1]) + pj[1][2]) + pj[1][3]);
-      if constexpr (OP)
-        if (kc + kAttnChunk > rq.L0 && (mask[t] & tree->bad)) S[t] = NAN;
       uint32_t hw[4], lw[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {   // keys 2 (e % 2), 2 (e % 2) + 1 of tile e / 2
@@ -244,15 +242,16 @@ __device__ __forceinline__ void tree_run(const AttnArgs& p, const TreeOp* op, Tr
 #pragma unroll
         for (int i = 0; i < 4; ++i) A[t][n][i] = A[t][n][i] * a + x[i] * c;
       }
-      if (!rows.valid(16 * (T * rp + t) + lr)) continue;
+      if (!rows.valid(row_of(t))) continue;
+      const int row = rq.row_start + rows.row(row_of(t)), h = rows.head(row_of(t));
       if (only) {   // one run holds every key
 #pragma unroll
         for (int n = 0; n < DT; ++n) {
           const float o[4] = {A[t][n][0] / S[t], A[t][n][1] / S[t], A[t][n][2] / S[t], A[t][n][3] / S[t]};
-          attn_store_out<true, D, false, 4>(p, OP ? op : nullptr, rq.row_start + row[t], h[t] * D + 16 * n + 4 * lg, o);
+          attn_store_out<true, D, false, 4>(p, OP ? op : nullptr, row, h * D + 16 * n + 4 * lg, o);
         }
       } else {
-        const size_t at = ((size_t)(rq.row_start + row[t]) * p.n_q + h[t]) * p.part_spans + j;
+        const size_t at = ((size_t)row * p.n_q + h) * p.part_spans + j;
 #pragma unroll
         for (int n = 0; n < DT; ++n) *gmem(reinterpret_cast<f4*>(p.pacc + at * D + 16 * n + 4 * lg)) = A[t][n];
         if (lg == 0) *gmem(reinterpret_cast<f2*>(p.pml + at * 2)) = f2{Mn, S[t]};
@@ -265,15 +264,13 @@ __device__ __forceinline__ void tree_run(const AttnArgs& p, const TreeOp* op, Tr
 // Items (run, KV head, row group) of one tree's rows from tensors, a run per
 // workgroup.
 template <int D, int T>
-__global__ __launch_bounds__(kTreeThreads, 2) void tree_op_kernel(const AttnArgs p, const TreeOp op) {
+__global__ __launch_bounds__(kTreeThreads, 2) void tree_op_kernel(const AttnArgs p, const TreeOp op, const int R, const int total) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ TreeLds tree;
   tree_masks_to_lds(op, &tree);
   __syncthreads();
   const ReqDesc rq = tree_req(op);
-  const int hpg = p.n_q / p.n_kv, ns = (rq.L0 + rq.W - 1) / kAttnSpanKeys + 1, per = (hpg * rq.W + 64 * T - 1) / (64 * T);
-  int R, total;
-  tree_runs(p, rq, 1, gridDim.x, T, R, total);
+  const int hpg = p.n_q / p.n_kv, ns = tree_spans(rq), per = TreeItems{p.n_kv, hpg, 64 * T}.per(rq);
   for (int t = xcd_contiguous(blockIdx.x, gridDim.x); t < total; t += gridDim.x) {
     const int j = t / (p.n_kv * per), v = t - j * p.n_kv * per, g = v / per, b = v - g * per;
     const AttnRows rows{g * hpg, rq.W, hpg * rq.W, b * 64 * T};
@@ -287,16 +284,14 @@ template <int D, int T>
 __global__ __launch_bounds__(kTreeThreads, 2) void tree_pass_kernel(const AttnArgs p, int n_reqs) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int hpg = p.n_q / p.n_kv;
+  const TreeItems items{p.n_kv, hpg, 64 * T};
   int R, total;
-  tree_runs(p, p.reqs, n_reqs, gridDim.x, T, R, total);
+  attn_run_length(p.reqs, n_reqs, gridDim.x, items, items, R, total);
   for (int t = xcd_contiguous(blockIdx.x, gridDim.x); t < total; t += gridDim.x) {
     int u = t, r = 0;
-    const auto per = [&](const ReqDesc& q) { return (hpg * q.W + 64 * T - 1) / (64 * T); };
-    const auto spans = [](const ReqDesc& q) { return (q.L0 + q.W - 1) / kAttnSpanKeys + 1; };
-    if (n_reqs > 1)
-      r = find_request(p.reqs, n_reqs, u, [&](const ReqDesc& q) { return p.n_kv * per(q) * ((spans(q) + R - 1) / R); });
+    if (n_reqs > 1) r = find_request(p.reqs, n_reqs, u, [&](const ReqDesc& q) { return items(q, R); });
     const ReqDesc rq = load_invariant(p.reqs + r);
-    const int n = per(rq), ns = spans(rq), j = u / (p.n_kv * n), v = u - j * p.n_kv * n, g = v / n, b = v - g * n;
+    const int n = items.per(rq), ns = tree_spans(rq), j = u / (p.n_kv * n), v = u - j * p.n_kv * n, g = v / n, b = v - g * n;
     const AttnRows rows{g * hpg, rq.W, hpg * rq.W, b * 64 * T};
     tree_run<D, T, false>(p, nullptr, nullptr, rq, rows, g, j * R, min((j + 1) * R, ns), j, R >= ns, smem);
   }
@@ -304,30 +299,32 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_pass_kernel(const AttnAr
 
 // The runs' states of a row and head joined in order, one wave each.
 template <int D>
-__global__ __launch_bounds__(64) void tree_op_join_kernel(const AttnArgs p, const TreeOp op, int T, int G) {
-  const ReqDesc rq = tree_req(op);
-  const int ns = (rq.L0 + rq.W - 1) / kAttnSpanKeys + 1, i = blockIdx.x / p.n_q;
-  int R, total;
-  tree_runs(p, rq, 1, G, T, R, total);
-  if (R < ns) attn_merge_wave<true, D>(p, rq, i, blockIdx.x - i * p.n_q, &op, (ns + R - 1) / R);
+__global__ __launch_bounds__(64) void tree_op_join_kernel(const AttnArgs p, const TreeOp op, const int runs) {
+  const int i = blockIdx.x / p.n_q;
+  attn_merge_wave<true, D>(p, tree_req(op), i, blockIdx.x - i * p.n_q, &op, runs);
 }
 template <int D>
 __global__ __launch_bounds__(64) void tree_pass_join_kernel(const AttnArgs p, int n_reqs, int T, int G) {
   int u = blockIdx.x, r = 0, R, total;
-  tree_runs(p, p.reqs, n_reqs, G, T, R, total);
+  const TreeItems items{p.n_kv, p.n_q / p.n_kv, 64 * T};
+  attn_run_length(p.reqs, n_reqs, G, items, items, R, total);
   if (n_reqs > 1) r = find_request(p.reqs, n_reqs, u, [&](const ReqDesc& q) { return q.W * p.n_q; });
   if (r < 0) return;
   const ReqDesc rq = load_invariant(p.reqs + r);
   if (u >= rq.W * p.n_q) return;
-  const int ns = (rq.L0 + rq.W - 1) / kAttnSpanKeys + 1, i = u / p.n_q;
+  const int ns = tree_spans(rq), i = u / p.n_q;
   if (R < ns) attn_merge_wave<true, D>(p, rq, i, u - i * p.n_q, nullptr, (ns + R - 1) / R);
 }
 
 template <int D, int T> static hipError_t tree_op(const AttnArgs& a, const TreeOp& op, int G, hipStream_t s) {
-  tree_op_kernel<D, T><<<G, kTreeThreads, tree_lds_bytes<D>(), s>>>(a, op);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  tree_op_join_kernel<D><<<op.W * a.n_q, 64, 0, s>>>(a, op, T, G);
+  const TreeItems items{a.n_kv, a.n_q / a.n_kv, 64 * T};
+  int R, total;
+  run_length_of(tree_req(op), G, items, items, R, total);
+  tree_op_kernel<D, T><<<std::min(G, total), kTreeThreads, tree_lds_bytes<D>(), s>>>(a, op, R, total);
+  const hipError_t e = hipGetLastError();
+  const int runs = (tree_spans(tree_req(op)) + R - 1) / R;
+  if (e != hipSuccess || runs == 1) return e;
+  tree_op_join_kernel<D><<<op.W * a.n_q, 64, 0, s>>>(a, op, runs);
   return hipGetLastError();
 }
 template <int D, int T> static hipError_t tree_pass(const AttnArgs& a, int n_reqs, int G, hipStream_t s) {

@@ -417,7 +417,7 @@ __device__ __forceinline__ void attn_run_length(const ReqDesc* reqs, int n_reqs,
 
 // The same of one request.
 template <class Items, class Groups>
-__device__ __forceinline__ void run_length_of(const ReqDesc& rq, int G, Items&& items, Groups&& groups, int& R, int& total) {
+__host__ __device__ __forceinline__ void run_length_of(const ReqDesc& rq, int G, Items&& items, Groups&& groups, int& R, int& total) {
   R = 1;
   total = items(rq, 1);
   if (total <= G) return;
@@ -426,7 +426,7 @@ __device__ __forceinline__ void run_length_of(const ReqDesc& rq, int G, Items&& 
   total = items(rq, R);
   while (total > G && total > least) total = items(rq, ++R);
 }
-__device__ __forceinline__ ReqDesc tree_req(const TreeOp& op) { return ReqDesc{0, op.W, op.L0, op.slot}; }
+__host__ __device__ __forceinline__ ReqDesc tree_req(const TreeOp& op) { return ReqDesc{0, op.W, op.L0, op.slot}; }
 
 // Workgroups are dealt to the 8 XCDs round-robin by linear index.  The
 // index v of the work a block takes: XCD j's blocks take one contiguous
