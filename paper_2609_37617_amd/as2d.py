@@ -2,7 +2,10 @@
 
 Argument marshalling only: every step of the verification path runs in the
 library's HIP kernels.  Importing this module does not touch the GPU;
-loading the library fails loudly if it has not been built.
+loading the library fails loudly if it has not been built.  Tensors on the
+device are torch's; a program that uses torch imports it before the library
+is loaded (before the first Model or Sampler), since both bring a HIP runtime
+and the first one serves the process.
 """
 import ctypes
 import os
@@ -342,7 +345,8 @@ class Model:
         """verify_tree with the candidates tested by sampling: `uniforms` has
         one number in [0, 1) per candidate and one for the token after the
         path; draft_logits (numpy or device float32, [rows, vocab]) the logits
-        that the children of each row were drawn from."""
+        that the children of each row were drawn from (device logits of the
+        current torch stream are waited for)."""
         return self._tree([req], [cands], None if parents is None else [parents],
                           [dict(uniforms=uniforms, temperature=temperature, draft_logits=draft_logits,
                                 draft_temperature=draft_temperature)])[0]
@@ -407,7 +411,9 @@ class Model:
         """Attention of a tree's rows over one layer of the request's cache
         (as2d_tree_attention): q [rows, n_q_heads, head_dim], k and v
         [rows, n_kv_heads, head_dim], device tensors of the model's type, on
-        the current torch stream or `stream`.  Returns out (new if None)."""
+        the current torch stream or `stream` (a handle; the caller then sees to
+        it that the tensors outlive the call's work).  Returns out (new if
+        None)."""
         s, rows, t = self.shape, q.shape[0], q.dtype
         if _types().get(t) != s.dtype:
             _refuse(f"tree_attention: {t} tensors, the model's type is {s.dtype}")
@@ -583,8 +589,9 @@ class Sampler:
         [n] int32, uniforms [n, k + 1] float32, temperature a number or a
         float32 tensor [n]: device tensors.  parents: a host list of k entries
         or None (chains).  Returns device tensors accepted [n], path [n, k],
-        token [n] and logp [n, k + 1], on the current torch stream or
-        `stream`."""
+        token [n] and logp [n, k + 1], on the current torch stream or `stream`
+        (a handle; the caller then sees to it that the tensors outlive the
+        call's work)."""
         import torch
         shape, t = getattr(logits, "shape", ()), getattr(logits, "dtype", None)
         if len(shape) != 3 or shape[1] < 1 or t not in _types():

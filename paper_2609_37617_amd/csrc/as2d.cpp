@@ -11,7 +11,6 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
-#include <functional>
 #include <map>
 #include <string>
 #include <tuple>
@@ -801,9 +800,11 @@ int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persi
 
 // One forward pass over the rows and requests in h_rows / h_reqs (see
 // launch_pass).  Verification passes run as a captured HIP graph (graph_for).
-// `after` launches what follows the pass before it is waited for.
+// `after` (a call, or null) launches what follows the pass before it is waited
+// for.
+template <class After = std::nullptr_t>
 int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool verify_call = false, PassRows tree = kPassVerify,
-                const std::function<int()>& after = nullptr) {
+                After&& after = nullptr) {
   join_op(c);
   const as2d_config& g = c->cfg;
   hipStream_t s = c->stream;
@@ -837,7 +838,7 @@ int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool v
                         : launch_pass(c, c->b, M, n_att, n_fin, fin_rows, with_head, max_blocks, !verify_call, tiles, tree);
     if (rc) return rc;
   }
-  if (after) {
+  if constexpr (!std::is_same_v<std::decay_t<After>, std::nullptr_t>) {
     const int rc = after();
     if (rc) return rc;
   }
@@ -1756,6 +1757,8 @@ int as2d_tree_attention(as2d_ctx* c, int32_t req, int32_t layer, int32_t n_rows,
   if ((rc = check_rows(c, "tree_attention", q)) || (rc = check_rows(c, "tree_attention", k)) ||
       (rc = check_rows(c, "tree_attention", v)) || (rc = check_rows(c, "tree_attention", out)))
     return rc;
+  if ((n_rows > 1 && out->row_stride < g.head_dim) || (g.n_q_heads > 1 && out->head_stride < g.head_dim))
+    return fail(c, AS2D_EINVAL, "tree_attention: rows or heads of out overlap");
   TreeOp op{};
   if ((rc = tree_masks(c, "tree_attention", parents, n_rows - 1, op.mask, nullptr, nullptr))) return rc;
   OnDevice on(c->dev);

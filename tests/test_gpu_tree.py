@@ -156,6 +156,7 @@ def test_attention_of_other_strides(served):
     shape, m = served
     keys, rows, parents = 333, 11, heap(10, 2)
     plain = attend_and_check(m, shape, keys, rows, parents, 3)
+    assert torch.equal(plain, attend_and_check(m, shape, keys, rows, np.array(parents), 3))
     heads_first = attend_and_check(m, shape, keys, rows, parents, 3,
                                    lambda x: x.transpose(0, 1).contiguous().transpose(0, 1))
 
@@ -170,6 +171,41 @@ def test_attention_of_other_strides(served):
     m.tree_attention(0, 1, q, k, v, parents, out=big[:, 1, :, 3:3 + shape.head_dim])
     assert torch.equal(big[:, 1, :, 3:3 + shape.head_dim], plain)
     assert not big[:, 0].any() and not big[:, 1, :, :3].any() and not big[:, 1, :, -2:].any()
+
+
+def test_keys_and_values_shared_by_all_rows(served):
+    """A broadcast input (stride 0) is read as it is."""
+    shape, m = served
+    q, k, v, K, V = tensors(shape, 6, 150, 4)
+    m.prefill(0, np.zeros(0, np.uint16), np.zeros(150, np.int32))
+    m.write_kv(0, 1, K, V)
+    one = m.tree_attention(0, 1, q, k[:1].expand(6, -1, -1), v[:1].expand(6, -1, -1), heap(5, 2))
+    copies = m.tree_attention(0, 1, q, k[:1].repeat(6, 1, 1), v[:1].repeat(6, 1, 1), heap(5, 2))
+    assert torch.equal(one, copies)
+
+
+def test_write_kv_before_a_pass(served):
+    """A pass on the context's stream waits for the rows another stream puts into the cache."""
+    shape, m = served
+    x = tensors(shape, 1, 3000, 9)[3:]
+    m.prefill(0, np.zeros(0, np.uint16), np.zeros(3000, np.int32))
+    state = m.state(0)
+    want = []
+    for K, V in (x, [t.flip(0) for t in x]):
+        for layer in range(2):
+            m.write_kv(0, layer, K, V)
+        torch.cuda.synchronize()
+        want.append(m.decode_one(0))
+        m.rollback(0, state[0], state[1])
+    side = torch.cuda.Stream()
+    for _ in range(4):
+        for w, (K, V) in zip(want, (x, [t.flip(0) for t in x])):
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                for layer in range(2):
+                    m.write_kv(0, layer, K, V)
+            assert m.decode_one(0) == w
+            m.rollback(0, state[0], state[1])
 
 
 def test_attention_on_streams_in_turn(served):
@@ -239,6 +275,7 @@ def test_operator_refusals(served):
     refused(as2d.EINVAL, att, 1, 0, q[:, :1], k, v)
     refused(as2d.EINVAL, att, 1, 0, q, k[:4], v)
     refused(as2d.EINVAL, att, 1, 0, q, k, v, out=torch.empty((5, 1, 1), device="cuda"))
+    refused(as2d.EINVAL, att, 1, 0, q, k, v, out=torch.empty_like(q[:1]).expand(5, -1, -1))
     refused(as2d.EINVAL, att, 1, 0, q.transpose(1, 2).contiguous().transpose(1, 2), k, v)
     big = tensors(shape, 33, 1, 0)
     refused(as2d.EINVAL, att, 1, 0, *big[:3])
