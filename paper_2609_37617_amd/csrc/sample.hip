@@ -23,8 +23,9 @@
 // MB: 1.1 us at a copy's 5.1 TB/s; 13.8 us in one launch: start 2.5, the pass
 // 2, the last workgroup's ticket and the rows' parts 3, tests 1, the token's
 // chunk and column 4); many rows, the pass over them (16 requests, 13 rows of
-// each that matter, 126 MB: 24 us, 5.3 TB/s, and 22 for the 64 nodes with a
-// second child, whose two rows are read again, and 15 to finish).
+// each that matter, 126 MB: 25 us, 5.1 TB/s, and 16 for those of the 64 nodes
+// with a second child whose first is rejected: their two rows are read again,
+// and 14 to finish).
 //
 // Rounding.  Exponentials are float32 (2^x by the hardware, about 1 unit in
 // the last place, with the argument's rounding put back: x is formed in 64
