@@ -138,6 +138,26 @@ def test_the_same_candidate_twice(sampler):
     check(sampler.verify(t, cands, u, parents=[-1] * 4), t, cands, u, [-1] * 4)
 
 
+def test_which_sibling_is_taken_from_call_to_call(sampler):
+    """A child's mass is left out where an earlier sibling is accepted: in calls
+    one after another on one workspace, what an earlier call left there has to
+    be neither read nor missed.  The number 0 accepts a child with anything
+    left; the last below 1 rejects most."""
+    k, branch, n = 12, 3, 6
+    parents = heap(k, branch)
+    t, d, cands, u = inputs(n, k, 5003, branch, seed=31, noise=1.5)
+    g = torch.Generator().manual_seed(5)
+    lengths = []
+    for first in (0, 3, 1, 3, 2, 0, None, None):   # the child that is given 0, 3: none, None: any
+        pick = torch.randint(0, 4, (n, k), generator=g) if first is None else torch.full((n, k), first)
+        turn = torch.arange(k) % branch   # which child of its node a candidate is
+        u[:, :k] = torch.where(pick == turn, 0.0, 1.0 - 2.0 ** -24).cuda()
+        got = sampler.verify(t, cands, u, parents=parents, draft_logits=d)
+        check(got, t, cands, u, parents, d)
+        lengths.append(got["accepted"].float().mean().item())
+    assert lengths[0] > lengths[1]     # the two kinds of call differ
+
+
 def test_candidates_outside_the_vocabulary_are_never_accepted(sampler):
     t, d, cands, u = inputs(1, 3, 60, 1, seed=8)
     cands[0] = torch.tensor([-1, 60, 2 ** 31 - 1], dtype=torch.int32)
