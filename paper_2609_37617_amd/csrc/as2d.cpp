@@ -174,16 +174,21 @@ int fail(as2d_ctx* c, int code, const char* fmt, ...) {
 #define HIP_TRY(c, expr)                                                                    \
   do {                                                                                      \
     hipError_t e_ = (expr);                                                                 \
-    if (e_ != hipSuccess)                                                                   \
+    if (e_ != hipSuccess) {                                                                 \
+      (void)hipGetLastError(); /* reported here: the next launch must not report it */      \
       return fail(c, e_ == hipErrorOutOfMemory ? AS2D_ENOMEM : AS2D_EHIP, "%s: %s (%s:%d)", \
                   #expr, hipGetErrorString(e_), __FILE__, __LINE__);                        \
+    }                                                                                       \
   } while (0)
 
 template <typename P>
 int dalloc(as2d_ctx* c, P** p, size_t bytes) {
   void* v = nullptr;
   hipError_t e = hipMalloc(&v, bytes ? bytes : 16);
-  if (e != hipSuccess) return fail(c, AS2D_ENOMEM, "hipMalloc(%zu): %s", bytes, hipGetErrorString(e));
+  if (e != hipSuccess) {
+    (void)hipGetLastError();   // the next launch must not report it
+    return fail(c, AS2D_ENOMEM, "hipMalloc(%zu): %s", bytes, hipGetErrorString(e));
+  }
   c->allocs.push_back(v);
   *p = static_cast<P*>(v);
   return AS2D_OK;
@@ -798,6 +803,17 @@ int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persi
   return AS2D_OK;
 }
 
+// Waits for the context's stream at the end of a scope that returns early: what
+// was launched or copied before an error still reads h_rows, h_reqs and the
+// caller's arrays.
+struct DrainOnError {
+  as2d_ctx* c;
+  bool armed = true;
+  ~DrainOnError() {
+    if (armed && hipStreamSynchronize(c->stream) != hipSuccess) (void)hipGetLastError();
+  }
+};
+
 // One forward pass over the rows and requests in h_rows / h_reqs (see
 // launch_pass).  Verification passes run as a captured HIP graph (graph_for).
 // `after` (a call, or null) launches what follows the pass before it is waited
@@ -817,6 +833,7 @@ int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool v
     max_blocks = std::max(max_blocks, (nk + kAttnBlock - 1) / kAttnBlock);
   }
   if (max_blocks > c->n_blocks_cap) return fail(c, AS2D_ECAPACITY, "attention blocks %d > %d", max_blocks, c->n_blocks_cap);
+  DrainOnError drain{c};
   const bool verify_pass = verify_call && with_head && n_fin == n_att;
   const bool persistent = verify_pass && tree == kPassVerify && c->exec_mode == AS2D_EXEC_PERSISTENT && c->pers_ok && c->pers_fit && M <= kStepRows;
   const bool graph = verify_pass && c->exec_mode != AS2D_EXEC_EAGER && !c->timing;
@@ -849,6 +866,7 @@ int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool v
     HIP_TRY(c, hipMemcpyAsync(c->h_margin, c->b.row_margin, sizeof(float) * M, hipMemcpyDeviceToHost, s));
   }
   HIP_TRY(c, hipStreamSynchronize(s));
+  drain.armed = false;
   timing_collect(c);
   if (persistent && c->h_err) {
     c->h_err = 0;
@@ -1093,12 +1111,28 @@ int grow(as2d_ctx* c, void** p, size_t* cap, size_t bytes) {
   return rc;
 }
 
+// Workspace of a pass's verification by sampling, before the pass is launched
+// (an allocation that fails then leaves nothing running).
+int reserve_sampling(as2d_ctx* c, int n, int max_k, int max_children, SampleArgs* a) {
+  a->vocab = c->cfg.vocab;
+  a->chunks = (a->vocab + kSampleChunk - 1) / kSampleChunk;
+  a->n = n;
+  a->k = max_k;
+  a->max_children = max_children;
+  const int mr = c->cfg.max_requests;
+  const size_t before = c->sample_cap;
+  const int rc = grow(c, &c->sample_work, &c->sample_cap, sample_layout(*a, mr, nullptr));
+  if (rc) return rc;
+  sample_layout(*a, mr, (char*)c->sample_work);
+  if (c->sample_cap != before) HIP_TRY(c, launch_fill_zero(a->ticket, mr, c->stream));
+  return AS2D_OK;
+}
+
 // Requests and drafter's logits of a sampling call to the device, before the
 // pass (the rows' order is h_rows'; row r of a request's logits belongs to its
 // row r, so only the rows up to the last one with children are there).
 int upload_sampling(as2d_ctx* c, int n, const int32_t* ks, const int32_t* parents, const as2d_sampling* sampling, bool draft) {
   const size_t V = c->cfg.vocab;
-  join_op(c);
   if (draft) {
     const ReqDesc& last = c->h_reqs[n - 1];
     const int rc = grow(c, (void**)&c->draft, &c->draft_cap, (size_t)(last.row_start + last.W) * V * 4);
@@ -1121,19 +1155,7 @@ int upload_sampling(as2d_ctx* c, int n, const int32_t* ks, const int32_t* parent
 }
 
 // Launches of a pass's verification by sampling, from the logits it left.
-int launch_sampling(as2d_ctx* c, int n, int max_k, int max_children, bool draft) {
-  SampleArgs a{};
-  a.vocab = c->cfg.vocab;
-  a.chunks = (a.vocab + kSampleChunk - 1) / kSampleChunk;
-  a.n = n;
-  a.k = max_k;
-  a.max_children = max_children;
-  const int mr = c->cfg.max_requests;
-  const size_t before = c->sample_cap;
-  const int rc = grow(c, &c->sample_work, &c->sample_cap, sample_layout(a, mr, nullptr));
-  if (rc) return rc;
-  sample_layout(a, mr, (char*)c->sample_work);
-  if (c->sample_cap != before) HIP_TRY(c, launch_fill_zero(a.ticket, mr, c->stream));
+int launch_sampling(as2d_ctx* c, SampleArgs a, bool draft) {
   a.target = c->b.logits;
   a.draft = draft ? c->draft : nullptr;
   a.t_stride = a.d_stride = c->cfg.vocab;
@@ -1677,6 +1699,7 @@ int as2d_verify_static(as2d_ctx* c, int32_t req, const int32_t* cands, int32_t k
                 need, cap, c->h_reqs[0].L0 + M);
   hipStream_t s = c->stream;
   join_op(c);
+  DrainOnError drain{c};
   // the array keeps the last call's contents: counters must start at zero
   HIP_TRY(c, launch_fill_zero(S.counters, (int)(S.attn_cnt - S.counters) + mr * g.n_q_heads * 2, s));
   const int timing = c->timing;   // no event bracketing here (events are created on first use)
@@ -1685,6 +1708,7 @@ int as2d_verify_static(as2d_ctx* c, int32_t req, const int32_t* cands, int32_t k
   c->timing = timing;
   if (rc) return rc;
   HIP_TRY(c, hipStreamSynchronize(s));
+  drain.armed = false;
   return commit_verify(c, 1, &req, &k, out);
 }
 
@@ -1706,12 +1730,17 @@ int as2d_verify_tree_batch(as2d_ctx* c, int32_t n, const int32_t* reqs, const in
   bool draft = false, chains = true;
   int max_children = 0, max_k = 0;
   if ((rc = assemble_tree(c, n, parents, ks, sampling, &max_k, &max_children, &draft, &chains))) return rc;
-  if (sampling && (rc = upload_sampling(c, n, ks, parents, sampling, draft))) return rc;
+  join_op(c);
+  SampleArgs sample{};
+  DrainOnError drain{c};
+  if (sampling && ((rc = reserve_sampling(c, n, max_k, max_children, &sample)) ||
+                   (rc = upload_sampling(c, n, ks, parents, sampling, draft))))
+    return rc;
   const int keep = c->keep_logits;
   if (sampling) c->keep_logits = 1;   // the pass writes the rows' logits
   rc = run_forward(c, M, n, n, true, true, chains ? kPassChains : kPassTrees, [&]() -> int {
     if (sampling) {
-      const int rc = launch_sampling(c, n, max_k, max_children, draft);
+      const int rc = launch_sampling(c, sample, draft);
       if (rc) return rc;
     }
     const as2d_config& g = c->cfg;
@@ -1722,6 +1751,7 @@ int as2d_verify_tree_batch(as2d_ctx* c, int32_t n, const int32_t* reqs, const in
   });
   c->keep_logits = keep;
   if (rc) return rc;
+  drain.armed = false;
   if (paths) {
     int off = 0;
     for (int r = 0; r < n; off += ks[r++])

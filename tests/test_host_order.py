@@ -1,0 +1,103 @@
+"""What the library's host code does, in which order, and after a call that
+fails: against a HIP runtime that runs nothing (tests/host)."""
+from dataclasses import replace
+
+import numpy as np
+import pytest
+
+from paper_2609_37617_amd import as2d
+from tests import host
+from workload import TINY_BF16, gen
+
+NARROW = replace(TINY_BF16, name="narrow", n_layers=2, hidden=128, ffn=64, vocab=128, qkv_bias=False)
+OWN_STREAM = 1000   # the context's stream: the first one made
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    path = host.build(str(tmp_path_factory.mktemp("host")))
+    saved, as2d._lib = as2d._lib, None
+    try:
+        yield as2d.load_library(path)
+    finally:
+        as2d._lib = saved
+
+
+@pytest.fixture
+def stub(lib, monkeypatch):
+    monkeypatch.setattr(as2d, "_lib", lib)
+    s = host.Stub(lib)
+    s.reset()
+    yield s
+    s.reset()
+
+
+@pytest.fixture
+def model(stub):
+    from workload.gen import _LIB_PATH
+    import os
+    if not os.path.exists(_LIB_PATH):
+        gen.build()
+    m = as2d.Model(NARROW, gen.make_weights(NARROW, 0, fmt="device"), max_requests=2, max_kv_len=256, max_k=31)
+    m.lib.as2d_set_exec_mode(m.ctx, as2d.EXEC_EAGER)
+    m.prefill(0, np.zeros(0, np.uint16), np.zeros(40, np.int32))
+    stub.log()
+    yield m
+    m.close()
+
+
+SAMPLED = dict(uniforms=np.full(5, 0.5, np.float32), parents=[-1, -1, 0, 0])
+CANDS = [1, 2, 3, 4]
+
+
+def launches(log):
+    return [line.split()[1] for line in log if line.startswith("launch")]
+
+
+def refused(code, f, *args, **kw):
+    with pytest.raises(as2d.As2dError) as e:
+        f(*args, **kw)
+    assert e.value.code == code, e.value
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_a_sampled_pass_without_memory_launches_nothing(model, stub, with_draft):
+    """The workspace is there before the pass starts, or the pass does not start."""
+    s = dict(SAMPLED, draft_logits=np.zeros((4, NARROW.vocab), np.float32) if with_draft else None)
+    state = model.state(0)
+    stub.malloc_limit(64)
+    refused(as2d.ENOMEM, model.verify_sampled, 0, CANDS, **s)
+    assert launches(stub.log()) == [] and model.state(0) == state
+    # the failed allocation is reported once, not by the next call's launches too
+    assert stub.pending_error() == 0
+    assert model.decode_one(0)["kv_len"] == state[0] + 1
+    stub.malloc_limit(-1)
+    stub.log()
+    model.verify_sampled(0, CANDS, **s)
+    log = stub.log()
+    assert launches(log)[0] == "fill_zero" and launches(log)[-2:] == ["sample", "move_path"]
+    assert log[-1] == f"sync {OWN_STREAM}"
+    assert "malloc" not in log[log.index(f"launch embed {OWN_STREAM}"):]
+
+
+@pytest.mark.parametrize("which", ["embed", "gemm", "attention", "finish", "tree_walk", "sample", "move_path"])
+def test_a_pass_that_fails_is_waited_for(model, stub, which):
+    """After an error nothing reads the descriptors or the caller's arrays any more, and the next call is as any other."""
+    state = model.state(0)
+    stub.fail_launch(which)
+    refused(as2d.EHIP, model.verify_sampled, 0, CANDS, draft_logits=np.zeros((4, NARROW.vocab), np.float32), **SAMPLED)
+    log = stub.log()
+    failed = next(i for i, line in enumerate(log) if line.endswith("failed"))
+    assert f"sync {OWN_STREAM}" in log[failed:] and model.state(0) == state and stub.pending_error() == 0
+    stub.fail_launch("")
+    assert model.verify_sampled(0, CANDS, **SAMPLED)["kv_len"] == state[0] + 1
+
+
+@pytest.mark.parametrize("which", ["embed", "attention", "finish"])
+def test_a_plain_pass_that_fails_is_waited_for(model, stub, which):
+    state = model.state(0)
+    stub.fail_launch(which)
+    refused(as2d.EHIP, model.verify, 0, CANDS)
+    assert stub.log()[-1] == f"sync {OWN_STREAM}" and model.state(0) == state
+    stub.fail_launch("")
+    assert model.verify(0, CANDS)["kv_len"] == state[0] + 1
