@@ -280,10 +280,12 @@ int as2d_write_kv(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t pos, int32_
  * <= 4096 requests, max_k <= 31 candidates and max_vocab <= 2^24 tokens on the
  * current device.  as2d_sampler_verify is ordered on hip_stream and returns
  * before it has run; it may be captured into a graph.  Calls of one sampler
- * share the workspace: calls on several streams are ordered by the library,
- * captured calls by whoever replays the graphs.  One host thread at a time.
- * Errors: AS2D_EINVAL, AS2D_EHIP, AS2D_ENOMEM; as2d_sampler_last_error(NULL) has
- * the message of a failed create.
+ * share the workspace: calls on several streams are ordered by the library
+ * (AS2D_ESTATE where the last call's stream is being captured by now: what ran
+ * there before cannot be waited for), captured calls by whoever replays the
+ * graphs.  One host thread at a time.  Errors: AS2D_EINVAL, AS2D_ESTATE,
+ * AS2D_EHIP, AS2D_ENOMEM; as2d_sampler_last_error(NULL) has the message of a
+ * failed create.
  */
 typedef struct as2d_sampler as2d_sampler;
 

@@ -37,6 +37,7 @@ int fail(as2d_sampler* s, int code, const char* fmt, ...) {
 }
 
 int hip_fail(as2d_sampler* s, const char* what, hipError_t e) {
+  (void)hipGetLastError();   // reported here: the next launch must not report it
   return fail(s, e == hipErrorOutOfMemory ? AS2D_ENOMEM : AS2D_EHIP, "sampler: %s: %s", what, hipGetErrorString(e));
 }
 
@@ -50,6 +51,17 @@ struct OnDevice {
     if (before >= 0) (void)hipSetDevice(before);
   }
 };
+
+// The workspace is the last call's until it has run: stream st waits for it.
+hipError_t after_last(as2d_sampler* s, hipStream_t st) {
+  hipStreamCaptureStatus before = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s->last, &before) == hipSuccess && before != hipStreamCaptureStatusNone)
+    return hipErrorStreamCaptureUnsupported;   // an event recorded there would be a node of the caller's graph
+  hipError_t e = hipEventRecord(s->ev, s->last);
+  e = e == hipSuccess ? hipStreamWaitEvent(st, s->ev, 0) : hipDeviceSynchronize();   // the stream may be gone
+  if (e == hipSuccess) (void)hipGetLastError();   // of the queries
+  return e;
+}
 
 }  // namespace
 
@@ -152,21 +164,16 @@ int as2d_sampler_verify(as2d_sampler* s, const as2d_sample_args* p, void* hip_st
   hipError_t e = st ? hipStreamGetDevice(st, &d) : hipSuccess;
   if (e != hipSuccess) return hip_fail(s, "stream", e);
   if (d != s->dev) return fail(s, AS2D_EINVAL, "sampler: the stream belongs to device %d, the sampler to %d", d, s->dev);
-  if (s->used && s->last != st) {
-    // the workspace is the last call's until it has run; a captured call is
-    // ordered by who replays the graph
-    hipStreamCaptureStatus now = hipStreamCaptureStatusNone, before = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(st, &now) == hipSuccess && now == hipStreamCaptureStatusNone &&
-        (hipStreamIsCapturing(s->last, &before) != hipSuccess || before == hipStreamCaptureStatusNone)) {
-      (void)hipGetLastError();
-      e = hipEventRecord(s->ev, s->last);
-      e = e == hipSuccess ? hipStreamWaitEvent(st, s->ev, 0) : hipDeviceSynchronize();   // the stream may be gone
-      if (e != hipSuccess) return hip_fail(s, "stream order", e);
-    }
-    (void)hipGetLastError();
+  hipStreamCaptureStatus now = hipStreamCaptureStatusNone;
+  if ((e = hipStreamIsCapturing(st, &now)) != hipSuccess) return hip_fail(s, "stream", e);
+  if (now == hipStreamCaptureStatusNone) {   // a captured call runs nothing now: it is ordered by who replays the graph
+    if (s->used && s->last != st && (e = after_last(s, st)) != hipSuccess)
+      return e == hipErrorStreamCaptureUnsupported
+                 ? fail(s, AS2D_ESTATE, "sampler: the last call's stream is being captured: that call cannot be waited for")
+                 : hip_fail(s, "stream order", e);
+    s->used = true;
+    s->last = st;
   }
-  s->used = true;
-  s->last = st;
   e = launch_sample(a, a.draft != nullptr, st);
   return e == hipSuccess ? AS2D_OK : hip_fail(s, "launch", e);
 }

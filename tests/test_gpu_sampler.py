@@ -317,3 +317,28 @@ def test_no_requests(sampler):
     got = sampler.verify(torch.empty((0, 4, 10), device="cuda"), torch.empty((0, 3), dtype=torch.int32, device="cuda"),
                          torch.empty((0, 4), device="cuda"))
     assert got["accepted"].shape == (0,) and got["path"].shape == (0, 3)
+
+
+def test_a_call_captured_while_another_runs(sampler):
+    """A long call runs on one stream while one is captured, and never
+    replayed, on a second; calls on the second and a third, of other shapes and
+    with nothing waited for, still come after the first."""
+    long, captured, short = (inputs(8, 8, 152064, 2, seed=23), inputs(2, 3, 9000, 1, seed=24), inputs(3, 5, 30000, 1, seed=25))
+    a, b, c = (torch.cuda.Stream() for _ in range(3))
+    sampler.verify(captured[0], captured[2], captured[3], draft_logits=captured[1])
+    for _ in range(3):
+        torch.cuda.synchronize()
+        graph, got = torch.cuda.CUDAGraph(), []
+        with torch.cuda.stream(a):
+            for _ in range(4):
+                got.append((sampler.verify(long[0], long[2], long[3], parents=heap(8, 2), draft_logits=long[1]), long, 2))
+        with torch.cuda.stream(b):
+            graph.capture_begin()
+            sampler.verify(captured[0], captured[2], captured[3], draft_logits=captured[1])
+            graph.capture_end()
+            got.append((sampler.verify(short[0], short[2], short[3], draft_logits=short[1]), short, 1))
+        with torch.cuda.stream(c):
+            got.append((sampler.verify(long[0], long[2], long[3], parents=heap(8, 2), draft_logits=long[1]), long, 2))
+        torch.cuda.synchronize()
+        for out, x, branch in got:
+            check(out, x[0], x[2], x[3], heap(x[2].shape[1], branch), x[1])

@@ -1,5 +1,6 @@
 """What the library's host code does, in which order, and after a call that
 fails: against a HIP runtime that runs nothing (tests/host)."""
+import ctypes
 from dataclasses import replace
 
 import numpy as np
@@ -101,3 +102,75 @@ def test_a_plain_pass_that_fails_is_waited_for(model, stub, which):
     assert stub.log()[-1] == f"sync {OWN_STREAM}" and model.state(0) == state
     stub.fail_launch("")
     assert model.verify(0, CANDS)["kv_len"] == state[0] + 1
+
+
+# ---------------------------------------------------------------------------
+# The sampler
+
+class HostSampler:
+    """Calls of a sampler on numbers as streams; the tensors are never read."""
+
+    def __init__(self, lib):
+        self.lib, self.h = lib, ctypes.c_void_p()
+        assert lib.as2d_sampler_create(2, 3, 500, ctypes.byref(self.h)) == as2d.OK
+
+    def verify(self, stream):
+        some = 4096   # an address nothing reads
+        a = as2d.SampleArgs(1, 2, 500, as2d.F32, some, 500, None, 0, some, None, None, some, None, 1.0, 0.0, some, some, some, None)
+        return self.lib.as2d_sampler_verify(self.h, a, stream)
+
+
+@pytest.fixture
+def sampler(stub):
+    s = HostSampler(stub.lib)
+    stub.log()
+    yield s
+    stub.lib.as2d_sampler_free(s.h)
+
+
+def order(log):
+    """Records, waits and launches, without the event's number."""
+    return [" ".join(w for i, w in enumerate(line.split()) if (line.split()[0], i) not in (("record", 1), ("wait", 2)))
+            for line in log if line.split()[0] in ("record", "wait", "launch", "sync")]
+
+
+def test_calls_on_several_streams_wait_for_the_last(sampler, stub):
+    for s, want in ((0, []), (0, []), (12, ["record 0", "wait 12"]), (12, []), (0, ["record 12", "wait 0"])):
+        assert sampler.verify(s) == as2d.OK
+        assert order(stub.log()) == want + [f"launch sample {s}"]
+
+
+def test_a_captured_call_does_not_hide_the_last_one_that_ran(sampler, stub):
+    """A call on 11 still runs; one is captured on 12, which runs nothing: the
+    next calls, on 12 and on 13, wait for 11's and for each other."""
+    assert sampler.verify(11) == as2d.OK
+    stub.log()
+    stub.stream(12, capturing=True)
+    assert sampler.verify(12) == as2d.OK
+    assert order(stub.log()) == ["launch sample 12"]   # nothing recorded, nothing waited for
+    stub.stream(12)
+    assert sampler.verify(12) == as2d.OK
+    assert order(stub.log()) == ["record 11", "wait 12", "launch sample 12"]
+    assert sampler.verify(13) == as2d.OK
+    assert order(stub.log()) == ["record 12", "wait 13", "launch sample 13"]
+
+
+def test_the_first_call_captured(sampler, stub):
+    stub.stream(12, capturing=True)
+    assert sampler.verify(12) == as2d.OK
+    assert sampler.verify(13) == as2d.OK
+    assert order(stub.log()) == ["launch sample 12", "launch sample 13"]
+
+
+def test_the_last_call_s_stream_is_captured_by_now(sampler, stub):
+    """Its earlier work cannot be waited for (a record there would join the graph): refused, until the capture ends."""
+    assert sampler.verify(11) == as2d.OK
+    stub.log()
+    stub.stream(11, capturing=True)
+    assert sampler.verify(13) == as2d.ESTATE
+    assert order(stub.log()) == []
+    assert sampler.verify(11) == as2d.OK   # captured: behind its stream's earlier work wherever it is replayed there
+    stub.stream(11)
+    stub.log()
+    assert sampler.verify(13) == as2d.OK
+    assert order(stub.log()) == ["record 11", "wait 13", "launch sample 13"]
