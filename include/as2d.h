@@ -225,7 +225,8 @@ int as2d_verify_tree_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const 
  * strides (in elements).  The call is ordered on hip_stream (NULL: the default
  * stream) of the context's device and returns before it has run; the
  * context's other calls wait for it, and these calls for each other, whatever
- * their streams.  They cannot be captured into a graph (AS2D_ESTATE).
+ * their streams.  They cannot be captured into a graph (AS2D_ESTATE; so do
+ * calls that would have to wait for one whose stream is being captured by now).
  *
  * as2d_tree_attention: attention of n_rows <= 32 rows of a tree (row 0 the
  * root; parents, host, n_rows - 1 entries or NULL, as above) over positions

@@ -353,15 +353,28 @@ struct OnDevice {
   }
 };
 
+// Whether a stream is being captured: what ran on it before can then not be
+// waited for (an event recorded there would be a node of the caller's graph,
+// and a host wait would end the capture with an error).
+bool being_captured(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();   // the stream may be gone
+  return false;
+}
+const char* const kOpCaptured = "the stream of the last operator on the cache is being captured: it cannot be waited for";
+
 // Waits for an operator that another call left running: every other call reads
 // or writes what it does.
-void join_op(as2d_ctx* c) {
-  if (!c->op_pending) return;
-  c->op_pending = false;
+int join_op(as2d_ctx* c) {
+  if (!c->op_pending) return AS2D_OK;
+  if (being_captured(c->op_stream)) return fail(c, AS2D_ESTATE, "%s", kOpCaptured);
   if (hipStreamSynchronize(c->op_stream) != hipSuccess) {   // the caller may have destroyed its stream
     (void)hipGetLastError();
-    (void)hipDeviceSynchronize();
+    HIP_TRY(c, hipDeviceSynchronize());
   }
+  c->op_pending = false;
+  return AS2D_OK;
 }
 
 // Before an operator's launches on stream s: after those of an earlier one on
@@ -376,8 +389,14 @@ int begin_op(as2d_ctx* c, hipStream_t s) {
   if (s) HIP_TRY(c, hipStreamGetDevice(s, &d));
   if (d != c->dev) return fail(c, AS2D_EINVAL, "the stream belongs to device %d, the context to %d", d, c->dev);
   if (c->op_pending && c->op_stream != s) {
-    if (hipEventRecord(c->op_ev, c->op_stream) == hipSuccess) HIP_TRY(c, hipStreamWaitEvent(s, c->op_ev, 0));
-    else join_op(c);
+    if (being_captured(c->op_stream)) return fail(c, AS2D_ESTATE, "%s", kOpCaptured);
+    if (hipEventRecord(c->op_ev, c->op_stream) == hipSuccess) {
+      HIP_TRY(c, hipStreamWaitEvent(s, c->op_ev, 0));
+    } else {
+      (void)hipGetLastError();
+      const int rc = join_op(c);
+      if (rc) return rc;
+    }
   }
   c->op_pending = true;
   c->op_stream = s;
@@ -821,7 +840,7 @@ struct DrainOnError {
 template <class After = std::nullptr_t>
 int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool verify_call = false, PassRows tree = kPassVerify,
                 After&& after = nullptr) {
-  join_op(c);
+  if (const int rc = join_op(c)) return rc;
   const as2d_config& g = c->cfg;
   hipStream_t s = c->stream;
   const int mr = g.max_requests;
@@ -1330,7 +1349,7 @@ const char* as2d_last_error(const as2d_ctx* c) {
 
 void as2d_free(as2d_ctx* c) {
   if (!c) return;
-  join_op(c);
+  (void)join_op(c);   // hipFree below waits for the device in any case
   if (c->stream) hipStreamSynchronize(c->stream);
   for (void* p : c->allocs) hipFree(p);
   if (c->h_rows) hipHostFree(c->h_rows);
@@ -1619,6 +1638,7 @@ int as2d_prefill_kv(as2d_ctx* c, int32_t req, const void* audio, int32_t n_audio
   if (total > g.max_kv_len) return fail(c, AS2D_ECAPACITY, "prefill: %d rows > max_kv_len %d", total, g.max_kv_len);
   for (int i = 0; i < n_instr; ++i)
     if (instr[i] < 0 || instr[i] >= g.vocab) return fail(c, AS2D_EINVAL, "prefill: token id %d out of range", instr[i]);
+  if ((rc = join_op(c))) return rc;
   ReqState& st = c->reqs[req];
   st = ReqState();
   if (n_audio) {
@@ -1698,7 +1718,7 @@ int as2d_verify_static(as2d_ctx* c, int32_t req, const int32_t* cands, int32_t k
     return fail(c, AS2D_ECAPACITY, "verify_static: the pass needs %zu bytes of static scratch, %zu available (%d keys)",
                 need, cap, c->h_reqs[0].L0 + M);
   hipStream_t s = c->stream;
-  join_op(c);
+  if ((rc = join_op(c))) return rc;
   DrainOnError drain{c};
   // the array keeps the last call's contents: counters must start at zero
   HIP_TRY(c, launch_fill_zero(S.counters, (int)(S.attn_cnt - S.counters) + mr * g.n_q_heads * 2, s));
@@ -1730,7 +1750,7 @@ int as2d_verify_tree_batch(as2d_ctx* c, int32_t n, const int32_t* reqs, const in
   bool draft = false, chains = true;
   int max_children = 0, max_k = 0;
   if ((rc = assemble_tree(c, n, parents, ks, sampling, &max_k, &max_children, &draft, &chains))) return rc;
-  join_op(c);
+  if ((rc = join_op(c))) return rc;
   SampleArgs sample{};
   DrainOnError drain{c};
   if (sampling && ((rc = reserve_sampling(c, n, max_k, max_children, &sample)) ||
@@ -1921,7 +1941,7 @@ int as2d_read_kv(as2d_ctx* c, int32_t req, int32_t layer, void* host_k, void* ho
   const as2d_config& g = c->cfg;
   if (layer < 0 || layer >= g.n_layers || n_tok < 0 || n_tok > g.max_kv_len || !host_k || !host_v)
     return fail(c, AS2D_EINVAL, "read_kv: bad arguments");
-  join_op(c);
+  if (const int rc = join_op(c)) return rc;
   HIP_TRY(c, hipStreamSynchronize(c->stream));
   const size_t d = (size_t)g.head_dim, cap = (size_t)c->kv_stride;
   float* ok = static_cast<float*>(host_k);
@@ -1963,7 +1983,7 @@ int as2d_read_kv(as2d_ctx* c, int32_t req, int32_t layer, void* host_k, void* ho
 int as2d_set_stream(as2d_ctx* c, void* hip_stream) {
   if (!c) return AS2D_EINVAL;
   if (hip_stream && stream_restricted((hipStream_t)hip_stream)) return fail(c, AS2D_EINVAL, "set_stream: %s", kRestrictedStream);
-  join_op(c);
+  if (const int rc = join_op(c)) return rc;
   HIP_TRY(c, hipStreamSynchronize(c->stream));
   drop_launch_state(c);
   if (c->own_stream) {
@@ -2073,7 +2093,7 @@ int as2d_time_gemm(as2d_ctx* c, int32_t which, int32_t rows, int32_t reps, doubl
     return c ? fail(c, AS2D_EINVAL, "time_gemm: bad arguments") : AS2D_EINVAL;
   const as2d_config& g = c->cfg;
   hipStream_t s = c->stream;
-  join_op(c);
+  if (const int rc = join_op(c)) return rc;
   // rows describe positions 0..rows-1 of slot 0: only the QKV epilogue reads
   // them (cache rows it overwrites are in bounds; their contents are garbage)
   for (int i = 0; i < rows; ++i) c->h_rows[i] = RowDesc{0, 0, std::min(i, g.max_kv_len - 1), 0, -1, std::min(i, g.max_kv_len - 1), 0, 0.f};

@@ -137,7 +137,7 @@ bool range_plan_ok(const GemmArgs&) { return true; }
 int step_ra_slice(bool, int, int) { return 0; }
 hipError_t step_occupancy(bool, int, int, int, int, int* n) { return *n = 0, hipSuccess; }   // no persistent step kernel
 hipError_t static_scratch(void** p, size_t* n) {
-  static char scratch[16];
+  static char scratch[4 << 20];
   return *p = scratch, *n = sizeof scratch, hipSuccess;
 }
 hipError_t launch_pack(bool, const void*, uint4*, int, int, int, int, hipStream_t s) { return launch("pack", s); }

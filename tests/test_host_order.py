@@ -174,3 +174,56 @@ def test_the_last_call_s_stream_is_captured_by_now(sampler, stub):
     stub.log()
     assert sampler.verify(13) == as2d.OK
     assert order(stub.log()) == ["record 11", "wait 13", "launch sample 13"]
+
+
+# ---------------------------------------------------------------------------
+# Operators on one layer of a cache
+
+SOME = 4096   # an address nothing reads
+
+
+def rows(row=NARROW.n_q_heads * NARROW.head_dim, head=NARROW.head_dim):
+    return as2d.Rows(SOME, row, head)
+
+
+def attend(m, stream, n_rows=3, out=None):
+    return m.call("as2d_tree_attention", 0, 0, n_rows, None, rows(), rows(), rows(), out or rows(), stream)
+
+
+def put(m, stream):
+    return m.call("as2d_write_kv", 0, 0, 0, 4, as2d.BF16, rows(), rows(), stream)
+
+
+def test_operators_on_several_streams_wait_for_each_other(model, stub):
+    assert put(model, 11) == as2d.OK
+    assert attend(model, 11) == as2d.OK
+    assert attend(model, 12) == as2d.OK
+    assert put(model, 0) == as2d.OK
+    assert order(stub.log()) == ["launch put_rows 11", "launch tree_attention 11", "record 11", "wait 12", "launch tree_attention 12",
+                                 "record 12", "wait 0", "launch put_rows 0"]
+    model.decode_one(0)
+    assert order(stub.log())[:2] == ["sync 0", f"launch embed {OWN_STREAM}"]
+    model.decode_one(0)
+    assert order(stub.log())[0] == f"launch embed {OWN_STREAM}"   # waited for once
+
+
+def test_an_operator_s_stream_that_is_captured_by_now(model, stub):
+    """Neither an event of it nor a host wait may reach into the caller's
+    capture: what would have to wait is refused, and the capture goes on."""
+    assert put(model, 11) == as2d.OK
+    stub.stream(11, capturing=True)
+    stub.log()
+    state = model.state(0)
+    assert attend(model, 12) == as2d.ESTATE
+    assert attend(model, 11) == as2d.ESTATE
+    for f, args in ((model.decode_one, (0,)), (model.verify, (0, CANDS)), (model.verify_tree, (0, CANDS)),
+                    (model.verify_static, (0, CANDS)), (model.read_kv, (0, 0, 8)), (model.set_stream, (13,)),
+                    (lambda: model.verify_sampled(0, CANDS, **SAMPLED), ()),
+                    (model.prefill, (0, np.zeros(0, np.uint16), np.zeros(5, np.int32)))):
+        refused(as2d.ESTATE, f, *args)
+    assert order(stub.log()) == [] and model.state(0) == state
+    stub.stream(11)
+    assert attend(model, 12) == as2d.OK
+    assert order(stub.log()) == ["record 11", "wait 12", "launch tree_attention 12"]
+    model.decode_one(0)
+    assert order(stub.log())[0] == "sync 12"
