@@ -227,6 +227,7 @@ int as2d_verify_tree_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const 
  * context's other calls wait for it, and these calls for each other, whatever
  * their streams.  They cannot be captured into a graph (AS2D_ESTATE; so do
  * calls that would have to wait for one whose stream is being captured by now).
+ * Streams restricted by a CU mask are refused, as in as2d_set_stream (AS2D_EINVAL).
  *
  * as2d_tree_attention: attention of n_rows <= 32 rows of a tree (row 0 the
  * root; parents, host, n_rows - 1 entries or NULL, as above) over positions
@@ -279,7 +280,8 @@ int as2d_write_kv(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t pos, int32_
  *
  * as2d_sampler_create allocates the workspace of calls of up to max_requests
  * <= 4096 requests, max_k <= 31 candidates and max_vocab <= 2^24 tokens on the
- * current device.  as2d_sampler_verify is ordered on hip_stream and returns
+ * current device.  as2d_sampler_verify is ordered on hip_stream (none that a CU
+ * mask restricts) and returns
  * before it has run; it may be captured into a graph.  Calls of one sampler
  * share the workspace: calls on several streams are ordered by the library
  * (AS2D_ESTATE where the last call's stream is being captured by now: what ran

@@ -220,26 +220,6 @@ GemmPlan make_plan(int N, int K, int KE, int target, int ks_override = 0) {
   return p;
 }
 
-// Whether a stream is confined to part of the device by a CU mask
-// (hipExtStreamCreateWithCUMask).  Such streams are refused: the first
-// concurrent run on masked streams ended in a host segmentation fault whose
-// cause has not been found, so the library never runs on one.  A stream
-// whose mask cannot be read is taken as unrestricted.
-const char* const kRestrictedStream =
-    "streams restricted by a CU mask are not supported (use as2d_set_cu_budget to share the device)";
-bool stream_restricted(hipStream_t s) {
-  int dev = 0, dev_cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&dev_cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || dev_cus < 1)
-    return false;
-  uint32_t mask[32] = {0};
-  const uint32_t words = (uint32_t)((dev_cus + 31) / 32);
-  if (words > 32 || hipExtStreamGetCUMask(s, words, mask) != hipSuccess) return false;
-  int n = 0;
-  for (uint32_t i = 0; i < words; ++i) n += __builtin_popcount(mask[i]);
-  return n > 0 && n < dev_cus;
-}
-
 // Workgroups of a balanced plan for `cus` compute units: one per CU, at
 // most one per unit, and at most kMaxUnits units each.  The split count is
 // not touched, so the sums do not change.
@@ -341,18 +321,6 @@ void timing_collect(as2d_ctx* c) {
   c->ev_used.clear();
 }
 
-// The calling thread's device, put back at the end of the scope.
-struct OnDevice {
-  int before = -1;
-  explicit OnDevice(int dev) {
-    int now = 0;
-    if (hipGetDevice(&now) == hipSuccess && now != dev && hipSetDevice(dev) == hipSuccess) before = now;
-  }
-  ~OnDevice() {
-    if (before >= 0) (void)hipSetDevice(before);
-  }
-};
-
 // Whether a stream is being captured: what ran on it before can then not be
 // waited for (an event recorded there would be a node of the caller's graph,
 // and a host wait would end the capture with an error).
@@ -388,6 +356,7 @@ int begin_op(as2d_ctx* c, hipStream_t s) {
   hipDevice_t d = c->dev;
   if (s) HIP_TRY(c, hipStreamGetDevice(s, &d));
   if (d != c->dev) return fail(c, AS2D_EINVAL, "the stream belongs to device %d, the context to %d", d, c->dev);
+  if (stream_restricted(s)) return fail(c, AS2D_EINVAL, "%s", kRestrictedStream);
   if (c->op_pending && c->op_stream != s) {
     if (being_captured(c->op_stream)) return fail(c, AS2D_ESTATE, "%s", kOpCaptured);
     if (hipEventRecord(c->op_ev, c->op_stream) == hipSuccess) {

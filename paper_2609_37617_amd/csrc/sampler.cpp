@@ -8,7 +8,7 @@
 #include <new>
 #include <string>
 
-#include "../../include/as2d.h"
+#include "internal.h"
 #include "kernels.h"
 
 using namespace as2d;
@@ -40,17 +40,6 @@ int hip_fail(as2d_sampler* s, const char* what, hipError_t e) {
   (void)hipGetLastError();   // reported here: the next launch must not report it
   return fail(s, e == hipErrorOutOfMemory ? AS2D_ENOMEM : AS2D_EHIP, "sampler: %s: %s", what, hipGetErrorString(e));
 }
-
-struct OnDevice {
-  int before = -1;
-  explicit OnDevice(int dev) {
-    int now = 0;
-    if (hipGetDevice(&now) == hipSuccess && now != dev && hipSetDevice(dev) == hipSuccess) before = now;
-  }
-  ~OnDevice() {
-    if (before >= 0) (void)hipSetDevice(before);
-  }
-};
 
 // The workspace is the last call's until it has run: stream st waits for it.
 hipError_t after_last(as2d_sampler* s, hipStream_t st) {
@@ -164,6 +153,7 @@ int as2d_sampler_verify(as2d_sampler* s, const as2d_sample_args* p, void* hip_st
   hipError_t e = st ? hipStreamGetDevice(st, &d) : hipSuccess;
   if (e != hipSuccess) return hip_fail(s, "stream", e);
   if (d != s->dev) return fail(s, AS2D_EINVAL, "sampler: the stream belongs to device %d, the sampler to %d", d, s->dev);
+  if (stream_restricted(st)) return fail(s, AS2D_EINVAL, "sampler: %s", kRestrictedStream);
   hipStreamCaptureStatus now = hipStreamCaptureStatusNone;
   if ((e = hipStreamIsCapturing(st, &now)) != hipSuccess) return hip_fail(s, "stream", e);
   if (now == hipStreamCaptureStatusNone) {   // a captured call runs nothing now: it is ordered by who replays the graph

@@ -227,3 +227,14 @@ def test_an_operator_s_stream_that_is_captured_by_now(model, stub):
     assert order(stub.log()) == ["record 11", "wait 12", "launch tree_attention 12"]
     model.decode_one(0)
     assert order(stub.log())[0] == "sync 12"
+
+
+def test_streams_restricted_by_a_mask_are_refused(model, sampler, stub):
+    """As as2d_set_stream refuses them: the library never runs on one."""
+    stub.stream(14, masked=True)
+    stub.log()
+    refused(as2d.EINVAL, model.set_stream, 14)
+    assert attend(model, 14) == put(model, 14) == sampler.verify(14) == as2d.EINVAL
+    assert stub.log() == []
+    assert attend(model, 15) == put(model, 15) == sampler.verify(15) == as2d.OK
+    assert order(stub.log()) == ["launch tree_attention 15", "launch put_rows 15", "launch sample 15"]
