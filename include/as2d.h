@@ -238,8 +238,9 @@ int as2d_verify_tree_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const 
  * as it is, later calls overwrite them; a row whose v is not finite is put as
  * 0).  A row of k or v that holds a NaN or an infinity reaches only the rows
  * that see it; such a v makes their whole head NaN.  kv_len + n_rows <=
- * max_kv_len (else AS2D_ECAPACITY).  out must not overlap q, k or v.  Passes
- * over trees run the same code on the rows of a pass.
+ * max_kv_len (else AS2D_ECAPACITY).  out must not overlap q, k or v, and its
+ * rows lie past each other's heads or its heads past each other's rows
+ * (AS2D_EINVAL).  Passes over trees run the same code on the rows of a pass.
  *
  * as2d_write_kv: keys (rotated) and values of positions pos .. pos + n_tok - 1
  * <= kv_len - 1 of the layer, [n_tok][n_kv_heads][head_dim] in `dtype`

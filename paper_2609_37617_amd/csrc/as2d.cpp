@@ -1776,7 +1776,11 @@ int as2d_tree_attention(as2d_ctx* c, int32_t req, int32_t layer, int32_t n_rows,
   if ((rc = check_rows(c, "tree_attention", q)) || (rc = check_rows(c, "tree_attention", k)) ||
       (rc = check_rows(c, "tree_attention", v)) || (rc = check_rows(c, "tree_attention", out)))
     return rc;
-  if ((n_rows > 1 && out->row_stride < g.head_dim) || (g.n_q_heads > 1 && out->head_stride < g.head_dim))
+  // each dimension alone, and one nested in the other: strides past both dimensions' own extents may still meet
+  const auto past = [&](int64_t a, int64_t b, int n) { return (__int128)a >= (__int128)b * (n - 1) + g.head_dim; };
+  if ((n_rows > 1 && out->row_stride < g.head_dim) || (g.n_q_heads > 1 && out->head_stride < g.head_dim) ||
+      (n_rows > 1 && g.n_q_heads > 1 && !past(out->row_stride, out->head_stride, g.n_q_heads) &&
+       !past(out->head_stride, out->row_stride, n_rows)))
     return fail(c, AS2D_EINVAL, "tree_attention: rows or heads of out overlap");
   TreeOp op{};
   if ((rc = tree_masks(c, "tree_attention", parents, n_rows - 1, op.mask, nullptr, nullptr))) return rc;

@@ -184,6 +184,21 @@ def test_keys_and_values_shared_by_all_rows(served):
     assert torch.equal(one, copies)
 
 
+def test_an_output_of_equal_strides_is_refused(served):
+    """Row 1 of head 0 would be row 0 of head 1; heads past the rows are an ordinary output."""
+    shape, m = served
+    q, k, v, K, V = tensors(shape, 5, 150, 4)
+    m.prefill(0, np.zeros(0, np.uint16), np.zeros(150, np.int32))
+    m.write_kv(0, 1, K, V)
+    d, nq = shape.head_dim, shape.n_q_heads
+    room = torch.zeros((nq + 5) * d, dtype=q.dtype, device="cuda")
+    with pytest.raises(as2d.As2dError) as e:
+        m.tree_attention(0, 1, q, k, v, out=room.as_strided((5, nq, d), (d, d, 1)))
+    assert e.value.code == as2d.EINVAL
+    out = torch.empty((nq, 5, d), dtype=q.dtype, device="cuda").transpose(0, 1)
+    assert torch.equal(m.tree_attention(0, 1, q, k, v, out=out), m.tree_attention(0, 1, q, k, v))
+
+
 def test_write_kv_before_a_pass(served):
     """A pass on the context's stream waits for the rows another stream puts into the cache."""
     shape, m = served

@@ -238,3 +238,21 @@ def test_streams_restricted_by_a_mask_are_refused(model, sampler, stub):
     assert stub.log() == []
     assert attend(model, 15) == put(model, 15) == sampler.verify(15) == as2d.OK
     assert order(stub.log()) == ["launch tree_attention 15", "launch put_rows 15", "launch sample 15"]
+
+
+@pytest.mark.parametrize("row,head,n_rows,good", [
+    ("nq d", "d", 3, True), ("nq d + 5", "d", 3, True), ("d", "3 d", 3, True), ("d + 1", "3 d + 3", 3, True),   # nested
+    ("0", "d", 1, True), ("d", "d", 1, True),                                     # one row: its stride is not used
+    ("0", "d", 3, False), ("nq d", "0", 3, False), ("nq d", "d - 1", 3, False),   # a dimension over itself
+    ("d", "d", 3, False), ("d", "d + 1", 3, False), ("nq d - 1", "d", 3, False),   # one over the other
+    ("d", "2 d", 3, False), ("d", "2 d", 2, True),                                # heads past two rows, not three
+    ("2 d", "2 d", 3, False), ("9223372036854775807", "d", 3, True), ("d", "9223372036854775807", 3, True),
+    ("9223372036854775807", "9223372036854775807", 3, False)])
+def test_an_output_whose_rows_and_heads_overlap_is_refused(model, stub, row, head, n_rows, good):
+    names = {"nq": NARROW.n_q_heads, "d": NARROW.head_dim}
+
+    def value(text):
+        return eval(text.replace("nq d", "nq * d").replace("2 d", "2 * d").replace("3 d", "3 * d"), names)
+    rc = attend(model, 11, n_rows, rows(value(row), value(head)))
+    assert rc == (as2d.OK if good else as2d.EINVAL)
+    assert launches(stub.log()) == (["tree_attention"] if good else [])
