@@ -220,8 +220,8 @@ int as2d_verify_tree_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const 
 /*
  * Operators on one layer of a request's cache, for programs that run layers of
  * their own beside the library (draft heads that read the target's cache,
- * caches that arrive from another process).  Tensors are device memory,
- * [rows][heads][head_dim] with adjacent dimensions and any row and head
+ * caches that arrive from another process).  Tensors are memory of the
+ * context's device (the current one at as2d_load_weights), [rows][heads][head_dim] with adjacent dimensions and any row and head
  * strides (in elements).  The call is ordered on hip_stream (NULL: the default
  * stream) of the context's device and returns before it has run; the
  * context's other calls wait for it, and these calls for each other, whatever
@@ -259,8 +259,8 @@ int as2d_write_kv(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t pos, int32_
 
 /*
  * Sampler: verification of drafted tokens against the target's probabilities
- * from given random numbers, on device tensors, for programs that have the
- * logits already.
+ * from given random numbers, on tensors of its device (the current one at its
+ * creation), for programs that have the logits already.
  *
  * Request r has rows r (k + 1) .. of logits: the root's and its candidates'.
  * p = softmax(logits / temperature) of a row; q = softmax(draft_logits /

@@ -219,12 +219,22 @@ def _rows(t, name: str, dtype, shape) -> Rows:
     return Rows(p, stride[0], stride[1])
 
 
-def _one_device(tensors) -> int:
-    dev = tensors[0].get_device()
+def _current_device(lib) -> int:
+    """The calling thread's device, from the runtime the library is linked to."""
+    dev = _I()
+    if lib.hipGetDevice(ctypes.byref(dev)) != 0:
+        raise As2dError(EHIP, "no device")
+    return dev.value
+
+
+def _device_of(tensors, owner: int) -> int:
+    """The tensors' device, which has to be that of the model or sampler: its
+    kernels run there, and torch's default stream is the same handle on every
+    device, so that the library could not tell."""
     for t in tensors:
-        if t.get_device() != dev:
-            _refuse("tensors on several devices")
-    return dev
+        if t.get_device() != owner:
+            _refuse(f"a tensor on device {t.get_device()}, the model or sampler is on {owner}")
+    return owner
 
 
 def _stream_of(device: int, stream: Optional[int]) -> int:
@@ -260,6 +270,7 @@ class Model:
         """shape: workload.configs.ModelShape; tensors: the canonical list
         in the 'device' format of workload.gen.make_weights."""
         self.lib = load_library()
+        self.device = _current_device(self.lib)
         self.shape = shape
         cfg = Config(shape.n_layers, shape.hidden, shape.n_q_heads, shape.n_kv_heads, shape.head_dim,
                      shape.ffn, shape.vocab, shape.rope_theta, shape.rms_eps, shape.dtype,
@@ -424,7 +435,8 @@ class Model:
             out = q.new_empty(q_shape)
         self._check(self.lib.as2d_tree_attention(
             self.ctx, req, layer, rows, _parents(parents, rows - 1), _rows(q, "q", t, q_shape), _rows(k, "k", t, kv_shape),
-            _rows(v, "v", t, kv_shape), _rows(out, "out", t, q_shape), _stream_of(_one_device((q, k, v, out)), stream)))
+            _rows(v, "v", t, kv_shape), _rows(out, "out", t, q_shape),
+            _stream_of(_device_of((q, k, v, out), self.device), stream)))
         return out
 
     def write_kv(self, req: int, layer: int, k, v, pos: int = 0, stream: Optional[int] = None):
@@ -434,7 +446,7 @@ class Model:
         if t not in _types():
             _refuse(f"k: float32 or bfloat16 is wanted, not {t}")
         a = [_rows(x, name, t, (k.shape[0], s.n_kv_heads, s.head_dim)) for x, name in ((k, "k"), (v, "v"))]
-        dev = _one_device((k, v))
+        dev = _device_of((k, v), self.device)
         if k.shape[0]:
             self._check(self.lib.as2d_write_kv(self.ctx, req, layer, pos, k.shape[0], _types()[t], *a, _stream_of(dev, stream)))
 
@@ -566,6 +578,7 @@ class Sampler:
 
     def __init__(self, max_requests: int, max_k: int, max_vocab: int):
         self.lib = load_library()
+        self.device = _current_device(self.lib)
         self.h = _P()
         rc = self.lib.as2d_sampler_create(max_requests, max_k, max_vocab, ctypes.byref(self.h))
         if rc != OK:
@@ -615,7 +628,7 @@ class Sampler:
             tensors.append(temperature)
             temperature = 0.0
         p_uniforms = _dense(uniforms, "uniforms", torch.float32, (n, rows))
-        dev = _one_device(tensors)
+        dev = _device_of(tensors, self.device)
         new = cands if k else uniforms.new_empty(0, dtype=torch.int32)
         out = dict(accepted=new.new_empty(n), path=new.new_empty((n, k)), token=new.new_empty(n),
                    logp=uniforms.new_empty((n, rows)))

@@ -67,6 +67,7 @@ void stub_clear_log() { g_log.clear(); }
 void stub_malloc_limit(long long bytes) { g_malloc_limit = bytes; }
 void stub_fail_launch(const char* name) { g_fail_launch = name; }
 void stub_stream(size_t s, int capturing, int masked, int device) { g_streams[s] = Stream{capturing != 0, masked != 0, device}; }
+int stub_device() { return g_device; }
 int stub_pending_error() { return g_error; }
 
 // ---- the runtime ----------------------------------------------------------------

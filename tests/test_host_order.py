@@ -256,3 +256,78 @@ def test_an_output_whose_rows_and_heads_overlap_is_refused(model, stub, row, hea
     rc = attend(model, 11, n_rows, rows(value(row), value(head)))
     assert rc == (as2d.OK if good else as2d.EINVAL)
     assert launches(stub.log()) == (["tree_attention"] if good else [])
+
+
+# ---------------------------------------------------------------------------
+# The binding
+
+class Tensor:
+    """What the binding asks of a device tensor."""
+    is_cuda = True
+
+    def __init__(self, shape, dtype, device=0):
+        self.shape, self.dtype, self.device = tuple(shape), dtype, device
+
+    def get_device(self):
+        return self.device
+
+    def data_ptr(self):
+        return SOME
+
+    def is_contiguous(self):
+        return True
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+    def new_empty(self, shape, dtype=None):
+        return Tensor(shape if isinstance(shape, tuple) else (shape,), dtype or self.dtype, self.device)
+
+
+def test_tensors_of_another_device_are_refused(model, stub):
+    """The default stream is the null handle on every device: on tensors of
+    another one the library would run its kernels on its own."""
+    torch = pytest.importorskip("torch")
+    bf16, nq, nkv, d = torch.bfloat16, NARROW.n_q_heads, NARROW.n_kv_heads, NARROW.head_dim
+    sampler = as2d.Sampler(2, 3, 500)
+
+    def calls(other, which=None):
+        def at(name):
+            return other if which in (None, name) else 0
+        q, out = Tensor((3, nq, d), bf16, at("q")), Tensor((3, nq, d), bf16, at("out"))
+        k, v = Tensor((3, nkv, d), bf16, at("k")), Tensor((3, nkv, d), bf16, at("v"))
+        yield "attention", lambda: model.tree_attention(0, 0, q, k, v, out=out, stream=0)
+        yield "write", lambda: model.write_kv(0, 0, k, v, stream=0)
+        t, dr = Tensor((2, 3, 500), torch.float32, at("logits")), Tensor((2, 3, 500), torch.float32, at("draft"))
+        c, u = Tensor((2, 2), torch.int32, at("cands")), Tensor((2, 3), torch.float32, at("uniforms"))
+        yield "sampler", lambda: sampler.verify(t, c, u, draft_logits=dr, stream=0)
+    stub.log()
+    for _, f in calls(1):
+        refused(as2d.EINVAL, f)
+    for which, ops in (("q", ["attention"]), ("out", ["attention"]), ("k", ["attention", "write"]), ("v", ["attention", "write"]),
+                       ("logits", ["sampler"]), ("draft", ["sampler"]), ("cands", ["sampler"]), ("uniforms", ["sampler"])):
+        for op, f in calls(1, which):
+            if op in ops:
+                refused(as2d.EINVAL, f)
+    assert stub.log() == []
+    for _, f in calls(0):
+        f()
+    assert launches(stub.log()) == ["tree_attention", "put_rows", "sample"]
+    sampler.close()
+
+
+def test_the_device_is_the_one_at_creation(model, stub):
+    """Another current device later changes nothing; streams of another device are refused."""
+    stub.lib.hipSetDevice(1)
+    torch = pytest.importorskip("torch")
+    sampler = as2d.Sampler(1, 0, 500)
+    assert (model.device, sampler.device) == (0, 1)
+    t, u = Tensor((1, 1, 500), torch.float32, 1), Tensor((1, 1), torch.float32, 1)
+    refused(as2d.EINVAL, sampler.verify, t, None, u, stream=11)   # a stream of device 0
+    stub.stream(16, device=1)
+    sampler.verify(t, None, u, stream=16)
+    k = Tensor((3, NARROW.n_kv_heads, NARROW.head_dim), torch.bfloat16)
+    refused(as2d.EINVAL, model.write_kv, 0, 0, k, k, stream=16)
+    model.write_kv(0, 0, k, k, stream=11)
+    assert stub.lib.stub_device() == 1
+    sampler.close()
