@@ -513,11 +513,14 @@ __device__ __forceinline__ void attn_span_chunks(const AttnArgs& p, const ReqDes
     for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[rt][e >> 2][e & 3]);
     mx = swap_combine<false>(mx, FMax{});
     mx = swap_combine<true>(mx, FMax{});
+    // no key with a score (hidden ones are -inf, the maximum passes over NaN):
+    // 2^(-inf - 0) = 0, and a NaN that the row sees stays one
+    const float ref = mx == -INFINITY ? 0.0f : mx;
     float pj[2][4];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pj[kt][i] = mx == -INFINITY ? 0.0f : exp2_hw(s[rt][kt][i] - mx);
+      for (int i = 0; i < 4; ++i) pj[kt][i] = exp2_hw(s[rt][kt][i] - ref);
     float sm = (((pj[0][0] + pj[0][1]) + pj[0][2]) + pj[0][3]) + (((pj[1][0] + pj[1][1]) + pj[1][2]) + pj[1][3]);
     sm = swap_combine<false>(sm, FAdd{});
     sm = swap_combine<true>(sm, FAdd{});

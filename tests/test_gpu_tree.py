@@ -136,6 +136,27 @@ def test_non_finite_rows_reach_only_the_rows_that_see_them(served, what, value):
             assert torch.isnan(got[sees]).any(-1).all()
 
 
+@pytest.mark.parametrize("keys", [32, 64, 96, 97, 126, 127, 128, 160, 2144, 2528])
+def test_a_key_of_nan_is_never_passed_over(served, keys):
+    """Also where the NaN is all that a row sees of its chunk of 32 keys, the
+    others being hidden: the maximum of their scores is then -inf."""
+    shape, m = served
+    # candidates 0 and 3 see little of the tree, 5 and 6 a long path
+    parents = [-1, 0, 1, -1, 2, 4, 5]
+    q, k, v, K, V = tensors(shape, 8, keys, 8)
+    m.prefill(0, np.zeros(0, np.uint16), np.zeros(keys, np.int32))
+    m.write_kv(0, 1, K, V)
+    clean = m.tree_attention(0, 1, q, k, v, parents)
+    assert torch.isfinite(clean).all()
+    for row in range(8):
+        bad = k.clone()
+        bad[row] = float("nan")
+        got = m.tree_attention(0, 1, q, bad, v, parents)
+        sees = trees.visible(parents)[:, row]
+        assert torch.equal(got[~sees], clean[~sees]), row
+        assert torch.isnan(got[sees]).all(), row
+
+
 LONG = [QWEN05B, QWEN7B]
 
 
