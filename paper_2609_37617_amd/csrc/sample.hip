@@ -27,11 +27,11 @@
 // with a second child whose first is rejected: their two rows are read again,
 // and 14 to finish).
 //
-// Rounding.  Exponentials are float32 (2^x by the hardware, about 1 unit in
-// the last place, with the argument's rounding put back: x is formed in 64
-// bits, 2^x = 2^float(x) (1 + (x - float(x)) ln 2)); what is summed over a row, compared or logged is 64
-// bits, so that a random number next to a border falls on the same side as in
-// exact arithmetic.
+// Rounding.  Powers are good to 2^-33.8 and everything summed over a row,
+// compared or logged has 64 bits, so that a random number falls on another side
+// of a border than in exact arithmetic only within 2^-33 of it: a draw from
+// 152,064 tokens then differs with a probability near 10^-6 (with float32 powers
+// it was 3 10^-4).
 #include "common.h"
 
 namespace as2d {
@@ -136,20 +136,26 @@ template <bool BF> __device__ __forceinline__ void load_chunk(const void* base, 
   }
 }
 
-// 2^(x c - top).  (x c - top as a pair of float32 instead of 64 bits: one pass
-// over 16 x 13 rows of 152,064 logits 28.3 us against 24.8.)
-__device__ __forceinline__ float power(float x, double c, double top) {
-  const double y = fmax(__builtin_fma((double)x, c, -top), -200.0);   // 2^-200 and less (x = -inf) are 0 in float32
-  const float f = (float)y;
-  return __builtin_amdgcn_exp2f(f) * __builtin_fmaf((float)(y - (double)f), (float)kLn2, 1.0f);
+// 2^(x c - top) in 64 bits: x c - top = n + f, |f| <= 1/2, and 2^f = 1 + f g(f),
+// g of degree 6 by weighted least squares (relative error 2^-33.8); 0 from
+// 2^-1075 on.
+__device__ __forceinline__ double power(float x, double c, double top) {
+  constexpr double kRound = 6755399441055744.0;   // 1.5 2^52: a sum's low bits are the nearest integer
+  constexpr double g[7] = {0.6931471805416539,    0.24022651075853424,   0.05550410962572529,  0.009618036910832413,
+                           0.0013333430786686678, 0.0001546711034876234, 1.5314946856354705e-05};
+  const double y = fmax(__builtin_fma((double)x, c, -top), -1100.0), t = y + kRound, f = y - (t - kRound);
+  double v = g[6];
+#pragma unroll
+  for (int i = 5; i >= 0; --i) v = __builtin_fma(v, f, g[i]);
+  return __builtin_amdgcn_ldexp(__builtin_fma(v, f, 1.0), (int)(uint32_t)__builtin_bit_cast(uint64_t, t));
 }
 
 // What is left of a column: max(p - C q, 0) from the two powers and the factors
 // 1 / sum and C / sum.  One rounding per operation wherever it is formed, so
 // that a chunk's sum is positive exactly where one of its columns is.
-__device__ __forceinline__ double left_of(float p, double ps, float q, double qs) {
+__device__ __forceinline__ double left_of(double p, double ps, double q, double qs) {
 #pragma clang fp contract(off)
-  return fmax((double)p * ps - (double)q * qs, 0.0);
+  return fmax(p * ps - q * qs, 0.0);
 }
 
 // ---- reductions: fixed trees, the same bits in every lane -------------------
@@ -256,7 +262,7 @@ template <bool COH> __device__ __forceinline__ RowStat row_stat(const SamplePart
   return RowStat{wave_sum64(s), top, __ballot(bad) != 0 || !(top > -INFINITY)};
 }
 __device__ __forceinline__ double prob(float x, const RowStat& t, double c) {
-  return x > -INFINITY ? exp2(__builtin_fma((double)x, c, -t.top)) / t.sum : 0.0;
+  return power(x, c, t.top) / t.sum;
 }
 // log p of a token in natural units, rounded once.
 __device__ __forceinline__ float log_prob(float x, double top, double log_sum, double c) {
@@ -293,7 +299,7 @@ template <bool BF> __device__ __forceinline__ SamplePart chunk_part(const void* 
   if (top > -INFINITY) {
 #pragma unroll
     for (int e = 0; e < kPer; e += 4)
-      s += (double)((power(x[e], c, top) + power(x[e + 1], c, top)) + (power(x[e + 2], c, top) + power(x[e + 3], c, top)));
+      s += (power(x[e], c, top) + power(x[e + 1], c, top)) + (power(x[e + 2], c, top) + power(x[e + 3], c, top));
     s = wave_sum64(s);
   }
   return SamplePart{s, top};
@@ -618,7 +624,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
             if (top > -INFINITY) {
 #pragma unroll
               for (int e = 0; e < kPer; ++e)
-                v += is_gone(ch * kSampleChunk + column<BF>(e)) ? 0.0 : (double)power(y[e], q.c, top);
+                v += is_gone(ch * kSampleChunk + column<BF>(e)) ? 0.0 : power(y[e], q.c, top);
             }
             v = wave_sum64(v);
           }
@@ -670,7 +676,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
         v = left_of(power(y, q.c, t.top), ps, power(logit<BF>(a.draft, drow + col), q.dc, d.top), qs);
       } else {
         const double top = load_part<FUSED>(part + chunk).top;
-        if (top > -INFINITY && !is_gone(col)) v = rescale((double)power(y, q.c, top), top, t.top);
+        if (top > -INFINITY && !is_gone(col)) v = rescale(power(y, q.c, top), top, t.top);
       }
     }
     const int who = find_in_run(v, [&](double) { return rest; }, s_find, nullptr);

@@ -342,3 +342,59 @@ def test_a_call_captured_while_another_runs(sampler):
         torch.cuda.synchronize()
         for out, x, branch in got:
             check(out, x[0], x[2], x[3], heap(x[2].shape[1], branch), x[1])
+
+
+def next_to_borders(p, n, near):
+    """n float32 numbers in [0, 1) that lie `near` (a range of distances) a border of the running sums of p, either side."""
+    run = np.cumsum(p)
+    run /= run[-1]
+    grid = np.round(run[:-1] * 2.0 ** 24)   # multiples of 2^-24 are float32 numbers
+    away = grid * 2.0 ** -24 - run[:-1]
+    pick = np.flatnonzero((np.abs(away) > near[0]) & (np.abs(away) < near[1]) & (grid < 2 ** 24))
+    assert len(pick) >= n
+    return (grid[pick[np.linspace(0, len(pick) - 1, n).astype(int)]] * 2.0 ** -24).astype(np.float32)
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+@pytest.mark.parametrize("dtype,temperature", [(torch.float32, 1.0), (torch.bfloat16, 0.7)])
+def test_tokens_next_to_the_borders_of_the_running_sum(sampler, dtype, temperature, with_draft):
+    """Numbers close to a border between two tokens.  A term p or q is off by
+    twice 2^-33.8 of itself (its power and its row's sum), so the running sum of
+    what is left, and the whole one, by 2 (1 + 1) 2^-33.8 each, and their
+    quotient by 8 2^-33.8 = 2^-30.8 over the mass S that is left.  With a drafter
+    that is what one rejection leaves."""
+    n, V = 64, 152064
+    t, d, cands, _ = inputs(1, 1, V, 1, dtype, seed=26, noise=1.5)
+    p = np.exp(trees.log_softmax(t[0, 0].double().cpu().numpy(), temperature))
+    if with_draft:
+        q = np.exp(trees.log_softmax(d[0, 0].double().cpu().numpy(), temperature))
+        x = int(np.argmax(q / p))   # rejected by the largest number: q > p
+        left = np.maximum(p - q, 0.0)
+    else:
+        x = int(np.argmin(p))
+        left = p.copy()
+        left[x] = 0.0
+    assert left.sum() > 0.2
+    us = next_to_borders(left, n, (2.0 ** -30.5 / left.sum(), 2.0 ** -26))
+    u = torch.tensor([[1 - 2.0 ** -24, w] for w in us], dtype=torch.float32, device="cuda")
+    tt = t.expand(n, -1, -1).contiguous()
+    dd = d.expand(n, -1, -1).contiguous() if with_draft else None
+    cc = torch.full((n, 1), x, dtype=torch.int32, device="cuda")
+    got = sampler.verify(tt, cc, u, draft_logits=dd, temperature=temperature)
+    assert not got["accepted"].any()
+    check(got, tt, cc, u, [-1], dd, temperature)
+
+
+@pytest.mark.parametrize("gap", [3.0, 8.0, 12.0])
+def test_log_probabilities_of_a_token_that_carries_the_row(sampler, gap):
+    """The sum of a row is as good as its terms: log p of a token near
+    certainty is right to its own rounding (2^-24) and 2^-33.8 of the sum."""
+    V = 50257
+    g = torch.Generator().manual_seed(27)
+    t = torch.randn((8, 1, V), generator=g)
+    t[:, 0, 77] = gap + np.log(V) + torch.rand(8, generator=g)
+    got = sampler.verify(t.cuda(), None, torch.full((8, 1), 0.5, device="cuda"))
+    for r in range(8):
+        lp = trees.log_softmax(t[r, 0].double().numpy(), 1.0)
+        token = int(got["token"][r])
+        assert abs(float(got["logp"][r, 0]) - lp[token]) <= 2.0 ** -24 * abs(lp[token]) + 2.0 ** -33
