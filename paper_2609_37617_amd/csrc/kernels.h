@@ -344,8 +344,8 @@ struct SampleReq {
 // Temperatures: x / T stays far inside 64 bits' range for every float32 x.
 constexpr double kLeastTemp = 1e-30, kMostTemp = 1e30;
 
-struct SamplePart {            // one chunk of a row: sum of 2^(x c - top), top the least integer >= every x c (-inf: all
-  double sum, top;             // -inf; NaN: a value is NaN or +inf)
+struct SamplePart {            // one chunk of a row: sum of 2^((x - top) c), top its largest logit (-inf: all are;
+  double sum, top;             // NaN: a value is NaN or +inf)
 };
 struct SampleArgs {
   const void* target;          // [rows][vocab], float32 or bf16
@@ -371,7 +371,7 @@ struct SampleArgs {
   // workspace
   SamplePart* part;            // [n][2][k + 1][chunks]
   double* stage;               // [max_children - 1][n][k + 1][chunks]
-  double* cut;                 // [max_children][n][k + 1]
+  double* cut;                 // [max_children - 1][n][k + 1]
   double* left;                // [n][chunks]
   int* ticket;                 // [n], zero between launches
 };

@@ -42,6 +42,31 @@ constexpr int kPer = kSampleChunk / 64;   // logits of a lane
 constexpr int kBlock = 256, kWide = 1024;  // threads: one pass over the logits, and the kernels that also combine parts
 constexpr double kLog2E = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
 
+// ---- powers -----------------------------------------------------------------
+
+// 2^(d c) of a difference d <= 0 of logits, c = log2(e) / temperature, in 64
+// bits: d c = n + f, |f| <= 1/2, and 2^f = 1 + f g(f), g of degree 6 by weighted
+// least squares (relative error 2^-33.8).  Differences, and not x c, because x c
+// has no bits left after the point where the temperature is small.
+struct Power {
+  double c, low;   // 2^(low c) is 0
+  __device__ explicit Power(double c) : c(c), low(-1100.0 * __builtin_amdgcn_rcp(c)) {}
+  __device__ __forceinline__ double operator()(double d) const {
+    constexpr double kRound = 6755399441055744.0;   // 1.5 2^52: a sum's low bits are the nearest integer
+    constexpr double g[7] = {0.6931471805416539,    0.24022651075853424,   0.05550410962572529,  0.009618036910832413,
+                             0.0013333430786686678, 0.0001546711034876234, 1.5314946856354705e-05};
+    d = fmax(d, low);
+    const double t = __builtin_fma(d, c, kRound);
+    const double f = __builtin_fma(d, c, kRound - t);
+    double v = g[6];
+#pragma unroll
+    for (int i = 5; i >= 0; --i) v = __builtin_fma(v, f, g[i]);
+    return __builtin_amdgcn_ldexp(__builtin_fma(v, f, 1.0), (int)(uint32_t)__builtin_bit_cast(uint64_t, t));
+  }
+  // of logit x relative to top, the largest of its row or chunk
+  __device__ __forceinline__ double operator()(float x, double top) const { return (*this)((double)x - top); }
+};
+
 // ---- requests ---------------------------------------------------------------
 
 struct Req {
@@ -136,20 +161,6 @@ template <bool BF> __device__ __forceinline__ void load_chunk(const void* base, 
   }
 }
 
-// 2^(x c - top) in 64 bits: x c - top = n + f, |f| <= 1/2, and 2^f = 1 + f g(f),
-// g of degree 6 by weighted least squares (relative error 2^-33.8); 0 from
-// 2^-1075 on.
-__device__ __forceinline__ double power(float x, double c, double top) {
-  constexpr double kRound = 6755399441055744.0;   // 1.5 2^52: a sum's low bits are the nearest integer
-  constexpr double g[7] = {0.6931471805416539,    0.24022651075853424,   0.05550410962572529,  0.009618036910832413,
-                           0.0013333430786686678, 0.0001546711034876234, 1.5314946856354705e-05};
-  const double y = fmax(__builtin_fma((double)x, c, -top), -1100.0), t = y + kRound, f = y - (t - kRound);
-  double v = g[6];
-#pragma unroll
-  for (int i = 5; i >= 0; --i) v = __builtin_fma(v, f, g[i]);
-  return __builtin_amdgcn_ldexp(__builtin_fma(v, f, 1.0), (int)(uint32_t)__builtin_bit_cast(uint64_t, t));
-}
-
 // What is left of a column: max(p - C q, 0) from the two powers and the factors
 // 1 / sum and C / sum.  One rounding per operation wherever it is formed, so
 // that a chunk's sum is positive exactly where one of its columns is.
@@ -215,12 +226,9 @@ __device__ __forceinline__ double* cut_of(const SampleArgs& a, int s, int r, int
   return a.cut + ((size_t)(s - 1) * a.n + r) * (a.k + 1) + row;
 }
 
-// v 2^(from - to), both integers, from <= to.
-__device__ __forceinline__ double rescale(double v, double from, double to) { return ldexp(v, (int)fmax(from - to, -2000.0)); }
-
-// A row's sum of 2^(x c - top) from its chunks' parts (their tops are integers,
-// so nothing is rounded but the sum); bad: a value that is no logit, or none
-// that is finite.  One wave, every lane gets them.
+// A row's sum of 2^((x - top) c) from its chunks' parts, top its largest
+// logit; bad: a value that is no logit, or none that is finite.  One wave,
+// every lane gets them.
 struct RowStat {
   double sum, top;
   int bad;
@@ -229,7 +237,7 @@ template <bool COH> __device__ __forceinline__ SamplePart load_part(const Sample
   if constexpr (COH) return SamplePart{ld_coherent(&p->sum), ld_coherent(&p->top)};
   else return *p;
 }
-template <bool COH> __device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks) {
+template <bool COH> __device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks, const Power& w) {
   const int lane = threadIdx.x & 63;
   constexpr int B = 4;   // a lane's first parts, kept (262,144 tokens: all of them)
   SamplePart p[B];
@@ -254,19 +262,19 @@ template <bool COH> __device__ __forceinline__ RowStat row_stat(const SamplePart
   double s = 0.0;
 #pragma unroll
   for (int i = 0; i < B; ++i)
-    if (p[i].top > -INFINITY) s += rescale(p[i].sum, p[i].top, top);
+    if (p[i].top > -INFINITY) s += p[i].sum * w(p[i].top - top);
   for (int i = 64 * B + lane; i < chunks; i += 64) {
     const SamplePart v = load_part<COH>(part + i);
-    if (v.top > -INFINITY) s += rescale(v.sum, v.top, top);
+    if (v.top > -INFINITY) s += v.sum * w(v.top - top);
   }
   return RowStat{wave_sum64(s), top, __ballot(bad) != 0 || !(top > -INFINITY)};
 }
-__device__ __forceinline__ double prob(float x, const RowStat& t, double c) {
-  return power(x, c, t.top) / t.sum;
+__device__ __forceinline__ double prob(float x, const RowStat& t, const Power& w) {
+  return w(x, t.top) / t.sum;
 }
 // log p of a token in natural units, rounded once.
 __device__ __forceinline__ float log_prob(float x, double top, double log_sum, double c) {
-  return x > -INFINITY ? (float)((__builtin_fma((double)x, c, -top) - log_sum) * kLn2) : -INFINITY;
+  return (float)((((double)x - top) * c - log_sum) * kLn2);
 }
 
 // A candidate's test from p(x), q(x), C and the mass S of what is left.  The
@@ -282,8 +290,8 @@ __device__ __forceinline__ bool accepts(float u, double mass, double q, double l
 
 // ---- kernels ----------------------------------------------------------------
 
-// A wave's chunk of a row: its sum and the top it is scaled by.
-template <bool BF> __device__ __forceinline__ SamplePart chunk_part(const void* base, long long row, int chunk, int vocab, double c) {
+// A wave's chunk of a row: its largest logit and its sum relative to that.
+template <bool BF> __device__ __forceinline__ SamplePart chunk_part(const void* base, long long row, int chunk, int vocab, const Power& w) {
   float x[kPer];
   load_chunk<BF>(base, row, chunk, vocab, x);
   float m = -INFINITY;
@@ -294,12 +302,12 @@ template <bool BF> __device__ __forceinline__ SamplePart chunk_part(const void* 
     m = fmaxf(m, x[e]);
   }
   m = wave_max(m);
-  const double top = __ballot(bad) != 0 ? (double)NAN : m > -INFINITY ? ceil((double)m * c) : -INFINITY;
+  const double top = __ballot(bad) != 0 ? NAN : m;
   double s = 0.0;
   if (top > -INFINITY) {
 #pragma unroll
     for (int e = 0; e < kPer; e += 4)
-      s += (power(x[e], c, top) + power(x[e + 1], c, top)) + (power(x[e + 2], c, top) + power(x[e + 3], c, top));
+      s += (w(x[e], top) + w(x[e + 1], top)) + (w(x[e + 2], top) + w(x[e + 3], top));
     s = wave_sum64(s);
   }
   return SamplePart{s, top};
@@ -317,20 +325,20 @@ __global__ __launch_bounds__(kBlock) void sample_stats_kernel(const SampleArgs a
   if (which && (q.drow0 < 0 || !children_of(lane_parent(a, q), row))) return;
   const SamplePart p =
       chunk_part<BF>(which ? a.draft : a.target, (which ? q.drow0 + row : q.row0 + row) * (which ? a.d_stride : a.t_stride),
-                     chunk, a.vocab, which ? q.dc : q.c);
+                     chunk, a.vocab, Power(which ? q.dc : q.c));
   if ((threadIdx.x & 63) == 0) part_of(a, r, which, row)[chunk] = p;
 }
 
 // Sum of max(p - C q, 0) over a wave's chunk; ps, qs: 1 / sum and C / sum.
 template <bool BF>
 __device__ __forceinline__ double chunk_left(const SampleArgs& a, long long trow, long long drow, int chunk, double top,
-                                             double c, double ps, double dtop, double dc, double qs) {
+                                             const Power& w, double ps, double dtop, const Power& dw, double qs) {
   float x[kPer], y[kPer];
   load_chunk<BF>(a.target, trow, chunk, a.vocab, x);
   load_chunk<BF>(a.draft, drow, chunk, a.vocab, y);
   double s = 0.0;
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) s += left_of(power(x[e], c, top), ps, power(y[e], dc, dtop), qs);
+  for (int e = 0; e < kPer; ++e) s += left_of(w(x[e], top), ps, dw(y[e], dtop), qs);
   return wave_sum64(s);
 }
 
@@ -353,7 +361,7 @@ __global__ __launch_bounds__(kWide) void sample_stage_kernel(const SampleArgs a,
   uint32_t children = children_of(lane_parent(a, q), row);
   if (__popc(children) <= s) return;
   if (wave < 2) {
-    const RowStat t = row_stat<false>(part_of(a, r, wave, row), a.chunks);
+    const RowStat t = row_stat<false>(part_of(a, r, wave, row), a.chunks, Power(wave ? q.dc : q.c));
     if (lane == 0) s_stat[wave] = t;
   } else if (wave == 2) {
     double cut = 0.0, mass = 1.0;   // before the s-th child
@@ -381,15 +389,15 @@ __global__ __launch_bounds__(kWide) void sample_stage_kernel(const SampleArgs a,
   const RowStat t = s_stat[0], d = s_stat[1];
   bool skip = s_cut < 0.0;
   if (!skip && !t.bad && !d.bad) {
-    const double qx = prob(s_dl, d, q.dc);
-    skip = accepts(s_u, s_mass, qx, share_left(prob(s_l, t, q.c), qx, s_cut));
+    const double qx = prob(s_dl, d, Power(q.dc));
+    skip = accepts(s_u, s_mass, qx, share_left(prob(s_l, t, Power(q.c)), qx, s_cut));
   }
   const double cut = s_cut + s_mass;
   if (blockIdx.x == 0 && threadIdx.x == 0) *cut_of(a, s, r, row) = skip ? -1.0 : cut;
   if (skip || chunk >= a.chunks) return;
   const double left = t.bad || d.bad ? 0.0
                                      : chunk_left<BF>(a, (q.row0 + row) * a.t_stride, (q.drow0 + row) * a.d_stride, chunk, t.top,
-                                                      q.c, 1.0 / t.sum, d.top, q.dc, cut / d.sum);
+                                                      Power(q.c), 1.0 / t.sum, d.top, Power(q.dc), cut / d.sum);
   if (lane == 0) stage_of(a, s, r, row)[chunk] = left;
 }
 
@@ -471,7 +479,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
     const uint32_t children = children_of(parent, row);
     if (!which && lane == 0) s_children[row] = children;
     if (which && (!drafted || !children)) continue;
-    const RowStat st = row_stat<FUSED>(part_of(a, r, which, row), a.chunks);
+    const RowStat st = row_stat<FUSED>(part_of(a, r, which, row), a.chunks, Power(which ? q.dc : q.c));
     if (lane == 0) {
       s_stat[which][row] = st;
       if (st.bad) s_bad = 1;
@@ -503,8 +511,8 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
     double mass = siblings ? s_left[lane] : 1.0;
     double p = 0.0, qx = 1.0;
     if (cand && !bad) {
-      p = prob(l, s_stat[0][parent], q.c);
-      if (drafted) qx = prob(dl, s_stat[1][parent], q.dc);
+      p = prob(l, s_stat[0][parent], Power(q.c));
+      if (drafted) qx = prob(dl, s_stat[1][parent], Power(q.dc));
     }
     double left = drafted ? share_left(p, qx, cut) : p;
     if (lane < 32) s_cand[lane] = x;
@@ -561,7 +569,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
     qs = taken / d.sum;
     double* out = a.left + (size_t)r * a.chunks;
     for (int chunk = block * kWavesW + wave; chunk < a.chunks; chunk += blocks * kWavesW) {
-      const double v = chunk_left<BF>(a, trow, drow, chunk, t.top, q.c, ps, d.top, q.dc, qs);
+      const double v = chunk_left<BF>(a, trow, drow, chunk, t.top, Power(q.c), ps, d.top, Power(q.dc), qs);
       if (lane == 0) st<true>(out + chunk, v);
     }
     if (blocks > 1) {
@@ -624,7 +632,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
             if (top > -INFINITY) {
 #pragma unroll
               for (int e = 0; e < kPer; ++e)
-                v += is_gone(ch * kSampleChunk + column<BF>(e)) ? 0.0 : power(y[e], q.c, top);
+                v += is_gone(ch * kSampleChunk + column<BF>(e)) ? 0.0 : Power(q.c)(y[e], top);
             }
             v = wave_sum64(v);
           }
@@ -637,7 +645,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
         double v = p.sum;
         for (uint32_t b = gone; b; b &= b - 1)
           if (chunk_of(__builtin_ctz(b)) == i) v = s_again[__builtin_ctz(b)];
-        return v > 0.0 ? rescale(v, p.top, t.top) : 0.0;
+        return v > 0.0 ? v * Power(q.c)(p.top - t.top) : 0.0;
       };
       // a run of chunks per thread (up to 1,048,576 tokens: one chunk)
       const int per = (a.chunks + kWide - 1) / kWide;
@@ -668,15 +676,18 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
     chunk = max(chunk, 0);
     // the chunk's columns, one per thread: each summed as its chunk's sum took it
     const int col = chunk * kSampleChunk + tid;
-    double v = 0.0;
+    double v = 0.0, top = 0.0;
     float y = -INFINITY;
+    if (!(taken > 0.0)) {   // relative to the chunk's largest logit, as its sum was
+      top = load_part<FUSED>(part + chunk).top;
+      rest /= Power(q.c)(top - t.top);
+    }
     if (col < a.vocab) {
       y = logit<BF>(a.target, trow + col);
       if (taken > 0.0) {
-        v = left_of(power(y, q.c, t.top), ps, power(logit<BF>(a.draft, drow + col), q.dc, d.top), qs);
-      } else {
-        const double top = load_part<FUSED>(part + chunk).top;
-        if (top > -INFINITY && !is_gone(col)) v = rescale(power(y, q.c, top), top, t.top);
+        v = left_of(Power(q.c)(y, t.top), ps, Power(q.dc)(logit<BF>(a.draft, drow + col), d.top), qs);
+      } else if (top > -INFINITY && !is_gone(col)) {
+        v = Power(q.c)(y, top);
       }
     }
     const int who = find_in_run(v, [&](double) { return rest; }, s_find, nullptr);
@@ -697,7 +708,7 @@ template <bool BF> __global__ __launch_bounds__(kWide) void sample_fused_kernel(
   if (row > q.k) return;
   if (q.ok) {
     if (chunk < a.chunks) {
-      const SamplePart p = chunk_part<BF>(a.target, (q.row0 + row) * a.t_stride, chunk, a.vocab, q.c);
+      const SamplePart p = chunk_part<BF>(a.target, (q.row0 + row) * a.t_stride, chunk, a.vocab, Power(q.c));
       if ((threadIdx.x & 63) == 0) {
         SamplePart* out = part_of(a, r, 0, row) + chunk;
         st<true>(&out->sum, p.sum);

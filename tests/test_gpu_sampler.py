@@ -398,3 +398,36 @@ def test_log_probabilities_of_a_token_that_carries_the_row(sampler, gap):
         lp = trees.log_softmax(t[r, 0].double().numpy(), 1.0)
         token = int(got["token"][r])
         assert abs(float(got["logp"][r, 0]) - lp[token]) <= 2.0 ** -24 * abs(lp[token]) + 2.0 ** -33
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+@pytest.mark.parametrize("temperature", [1e-30, 1e-25, 1e-18, 1e-15, 1e-10, 1e-4, 1e4, 1e10, 1e30])
+def test_the_whole_range_of_temperatures(sampler, temperature, with_draft):
+    """From the largest logit alone to all tokens alike, over several chunks,
+    with two tokens that share the largest logit."""
+    n, k, V = 6, 3, 5000
+    t, d, cands, u = inputs(n, k, V, 1, seed=28, spread=20.0)
+    t[0, 0, [17, 4400]] = 200.0
+    d[1, 0, [18, 19]] = 200.0
+    cands[0, 0], cands[1, 0] = 4400, 19
+    t[2, 0, :] = -1.0e30   # far logits: a difference of 1 is none in float32
+    t[2, 0, 3000] = 2.0e37
+    t[3, 1, 5:] = -float("inf")
+    d = d if with_draft else None
+    got = sampler.verify(t, cands, u, draft_logits=d, temperature=temperature)
+    check(got, t, cands, u, trees.chain(k), d, temperature)
+
+
+@pytest.mark.parametrize("top", [1e4, 1e20, 1e38])
+def test_logits_of_any_size(sampler, top):
+    """Equal large logits and ones a few float32 steps below them."""
+    V, n = 3000, 5
+    step = float(np.spacing(np.float32(top)))
+    t = torch.full((n, 1, V), top)
+    t[:, 0] -= step * torch.randint(0, 9, (n, V), generator=torch.Generator().manual_seed(29))
+    u = torch.tensor([[0.0], [0.2], [0.5], [0.9], [1 - 2.0 ** -24]])
+    for temperature in (step, 20 * step):
+        if not 1e-30 <= temperature <= 1e30:
+            continue
+        check(sampler.verify(t.cuda(), None, u.cuda(), temperature=temperature), t, torch.zeros((n, 0), dtype=torch.int32), u, [],
+              None, temperature)
