@@ -227,17 +227,24 @@ __device__ __forceinline__ double* cut_of(const SampleArgs& a, int s, int r, int
 }
 
 // A row's sum of 2^((x - top) c) from its chunks' parts, top its largest
-// logit; bad: a value that is no logit, or none that is finite.  One wave,
-// every lane gets them.
+// logit; bad: a value that is no logit, or none that is finite.  rest: the sum
+// without the chunks that lanes `gone` (bits) have in `ours`.  One wave, every
+// lane gets them.
 struct RowStat {
-  double sum, top;
+  double sum, top, rest;
   int bad;
 };
 template <bool COH> __device__ __forceinline__ SamplePart load_part(const SamplePart* p) {
   if constexpr (COH) return SamplePart{ld_coherent(&p->sum), ld_coherent(&p->top)};
   else return *p;
 }
-template <bool COH> __device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks, const Power& w) {
+__device__ __forceinline__ bool one_of(int chunk, int ours, uint32_t gone) {
+  bool is = false;
+  for (uint32_t b = gone; b; b &= b - 1) is |= __builtin_amdgcn_readlane(ours, __builtin_ctz(b)) == chunk;
+  return is;
+}
+template <bool COH>
+__device__ __forceinline__ RowStat row_stat(const SamplePart* part, int chunks, const Power& w, int ours = -1, uint32_t gone = 0) {
   const int lane = threadIdx.x & 63;
   constexpr int B = 4;   // a lane's first parts, kept (262,144 tokens: all of them)
   SamplePart p[B];
@@ -259,15 +266,23 @@ template <bool COH> __device__ __forceinline__ RowStat row_stat(const SamplePart
     top = fmax(top, t);
   }
   top = wave_max64(top);
-  double s = 0.0;
+  double s = 0.0, rest = 0.0;
+  const auto add = [&](const SamplePart& v, int chunk) {   // by every lane: one_of reads the others' candidates
+    const bool is = gone && one_of(chunk, ours, gone);
+    if (!(v.top > -INFINITY)) return;
+    const double x = v.sum * w(v.top - top);
+    s += x;
+    rest += is ? 0.0 : x;
+  };
 #pragma unroll
-  for (int i = 0; i < B; ++i)
-    if (p[i].top > -INFINITY) s += p[i].sum * w(p[i].top - top);
-  for (int i = 64 * B + lane; i < chunks; i += 64) {
-    const SamplePart v = load_part<COH>(part + i);
-    if (v.top > -INFINITY) s += v.sum * w(v.top - top);
+  for (int i = 0; i < B; ++i) add(p[i], 64 * i + lane);
+  for (int i0 = 64 * B; i0 < chunks; i0 += 64) {
+    SamplePart v{0.0, -INFINITY};
+    if (i0 + lane < chunks) v = load_part<COH>(part + i0 + lane);
+    add(v, i0 + lane);
   }
-  return RowStat{wave_sum64(s), top, __ballot(bad) != 0 || !(top > -INFINITY)};
+  s = wave_sum64(s);
+  return RowStat{s, top, gone ? wave_sum64(rest) : s, __ballot(bad) != 0 || !(top > -INFINITY)};
 }
 __device__ __forceinline__ double prob(float x, const RowStat& t, const Power& w) {
   return w(x, t.top) / t.sum;
@@ -311,6 +326,30 @@ template <bool BF> __device__ __forceinline__ SamplePart chunk_part(const void* 
     s = wave_sum64(s);
   }
   return SamplePart{s, top};
+}
+
+// Chunk of the vocabulary of a candidate.
+__device__ __forceinline__ int chunk_of(int x, int vocab) { return x >= 0 && x < vocab ? x / kSampleChunk : -1; }
+// A rejected candidate's chunk without the rejected tokens (x: lane i's
+// candidate, gone: those of one node), 0 where an earlier one of them has the
+// chunk; one wave.
+template <bool BF, bool COH>
+__device__ __forceinline__ SamplePart chunk_rest(const SampleArgs& a, long long row, const SamplePart* part, const Power& w, int x, int i,
+                                                 uint32_t gone) {
+  const int ours = chunk_of(x, a.vocab), ch = __builtin_amdgcn_readlane(ours, i);
+  const uint32_t same = (uint32_t)__ballot(ours == ch) & gone;
+  if (ch < 0 || __builtin_ctz(same) != i) return SamplePart{0.0, -INFINITY};
+  float y[kPer];
+  load_chunk<BF>(a.target, row, ch, a.vocab, y);
+  const double top = load_part<COH>(part + ch).top;
+  if (!(top > -INFINITY)) return SamplePart{0.0, -INFINITY};
+  double v = 0.0;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) v += one_of(ch * kSampleChunk + column<BF>(e), x, same) ? 0.0 : w(y[e], top);
+  return SamplePart{wave_sum64(v), top};
+}
+__device__ __forceinline__ uint32_t but_last(uint32_t children) {
+  return children ? children & ~(0x80000000u >> __builtin_clz(children)) : 0;
 }
 
 // The parts of every chunk of the target's rows and of the drafter's rows with
@@ -451,6 +490,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
   constexpr int kWavesW = kWide / 64;
   __shared__ RowStat s_stat[2][32];
   __shared__ double s_left[32], s_again[32], s_log[32];
+  __shared__ SamplePart s_rest[32];
   __shared__ uint32_t s_children[32];
   __shared__ int s_cand[32], s_bad, s_at, s_n, s_path[32], s_last;
   __shared__ double s_cut, s_cutoff[32];
@@ -463,23 +503,42 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
   // candidates: what they need from memory, in flight while the rows' parts are combined
   const bool cand = wave < 2 && lane >= 1 && lane <= q.k;   // wave 0: the tests, wave 1: log-probabilities
   const float u_tok = uniform_of(a, q, 0);
+  const bool several = !drafted && a.max_children > 1;
   int x = -1;
   float u = 0.f, l = -INFINITY, dl = -INFINITY;
+  if ((cand || several) && lane >= 1 && lane <= q.k) x = cand_of(a, q, lane);
   if (cand) {
-    x = cand_of(a, q, lane);
     u = uniform_of(a, q, lane);
     if (x >= 0 && x < a.vocab) {
       l = logit<BF>(a.target, (q.row0 + parent) * a.t_stride + x);
       if (drafted) dl = logit<BF>(a.draft, (q.drow0 + parent) * a.d_stride + x);
     }
   }
+  if (several)
+    for (int i = 1 + wave; i <= q.k; i += kWavesW) {
+      const int p = __shfl(parent, i);
+      const uint32_t gone = but_last(children_of(parent, p));
+      if (!(gone >> i & 1)) continue;
+      const SamplePart v = chunk_rest<BF, FUSED>(a, (q.row0 + p) * a.t_stride, part_of(a, r, 0, p), Power(q.c), x, i, gone);
+      if (lane == 0) s_rest[i] = v;
+    }
   __syncthreads();
   for (int w = wave; w < 2 * (q.k + 1) && q.ok; w += kWavesW) {
     const int which = w > q.k, row = w - which * (q.k + 1);
     const uint32_t children = children_of(parent, row);
     if (!which && lane == 0) s_children[row] = children;
     if (which && (!drafted || !children)) continue;
-    const RowStat st = row_stat<FUSED>(part_of(a, r, which, row), a.chunks, Power(which ? q.dc : q.c));
+    // Without a drafter's row: what is left once every child but the last is
+    // rejected, summed from what is left (1 less their probabilities would have
+    // nothing but roundings where a child is near certain).
+    const uint32_t gone = several ? but_last(children) : 0;
+    const bool mine = lane < 32 && gone >> (lane & 31) & 1;
+    const Power pw(which ? q.dc : q.c);
+    RowStat st = row_stat<FUSED>(part_of(a, r, which, row), a.chunks, pw, chunk_of(x, a.vocab), gone);
+    if (gone) {
+      const SamplePart v = mine ? s_rest[lane] : SamplePart{0.0, -INFINITY};
+      st.rest += wave_sum64(v.top > -INFINITY ? v.sum * pw(v.top - st.top) : 0.0);
+    }
     if (lane == 0) {
       s_stat[which][row] = st;
       if (st.bad) s_bad = 1;
@@ -520,9 +579,9 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
     for (uint32_t b = before; b; b &= b - 1)   // a sibling that was rejected has taken the token
       if (s_cand[__builtin_ctz(b)] == x) left = 0.0;
     if (lane < 32) s_left[lane] = left;
-    if (!drafted) {
-      for (; before; before &= before - 1) mass -= s_left[__builtin_ctz(before)];
-      mass = fmax(mass, 0.0);
+    if (before) {   // what all children but the last leave, and those of them that are not tried yet
+      mass = s_stat[0][parent].rest / s_stat[0][parent].sum;
+      for (uint32_t b = but_last(s_children[parent]) & ~((1u << lane) - 1); b; b &= b - 1) mass += s_left[__builtin_ctz(b)];
     }
     const bool yes = cand && !bad && accepts(u, mass, qx, left);
     const uint32_t accepted = (uint32_t)__ballot(yes);
@@ -609,10 +668,6 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
       for (uint32_t b = gone; b; b &= b - 1) g |= s_cand[__builtin_ctz(b)] == col;
       return g;
     };
-    const auto chunk_of = [&](int row) {
-      const int c = s_cand[row];
-      return c >= 0 && c < a.vocab ? c / kSampleChunk : -1;
-    };
     int chunk = -1;
     double rest = 0.0;
     for (int round = 0; round < 2 && chunk < 0; ++round) {
@@ -623,7 +678,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
       // chunks of rejected tokens are summed again without them, a wave each
       for (int i = wave; i <= q.k; i += kWavesW)
         if (gone >> i & 1) {
-          const int ch = chunk_of(i);
+          const int ch = chunk_of(s_cand[i], a.vocab);
           double v = 0.0;
           if (ch >= 0) {
             float y[kPer];
@@ -644,7 +699,7 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
         const SamplePart p = load_part<FUSED>(part + i);
         double v = p.sum;
         for (uint32_t b = gone; b; b &= b - 1)
-          if (chunk_of(__builtin_ctz(b)) == i) v = s_again[__builtin_ctz(b)];
+          if (chunk_of(s_cand[__builtin_ctz(b)], a.vocab) == i) v = s_again[__builtin_ctz(b)];
         return v > 0.0 ? v * Power(q.c)(p.top - t.top) : 0.0;
       };
       // a run of chunks per thread (up to 1,048,576 tokens: one chunk)

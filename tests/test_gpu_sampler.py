@@ -431,3 +431,42 @@ def test_logits_of_any_size(sampler, top):
             continue
         check(sampler.verify(t.cuda(), None, u.cuda(), temperature=temperature), t, torch.zeros((n, 0), dtype=torch.int32), u, [],
               None, temperature)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V", [(24, 3000), (24, 50257)])
+@pytest.mark.parametrize("tokens", [[5, 6, 900, 901], [5, 2900, 1500, 10], [5, 5, 2900, 5], [2000, -1, 2047, 2048], [7, 2999, 2999, 8]])
+def test_children_after_near_certain_ones(sampler, dtype, n, V, tokens):
+    """Without a drafter's distribution the first two children have all but
+    10^-7 each of what is left at their turn; the others share the rest, with
+    numbers within 2^-20 of their borders.  In one workgroup's chunk of the
+    vocabulary and in several, repeated and outside the vocabulary."""
+    g = torch.Generator().manual_seed(30)
+    t = torch.randn((1, 5, V), generator=g)
+    large = [x for x in dict.fromkeys(tokens) if x >= 0]
+    # about e^16 of the sum of what comes after, each time
+    for i, x in enumerate(reversed(large[:2])):
+        t[0, 0, x] = 16.6 * (i + 1) + np.log(V) + 0.5
+    for x in large[2:]:
+        t[0, 0, x] = np.log(V) - 1.0 if dtype == torch.float32 else 10.0
+    t = t.to(dtype).expand(n, -1, -1).contiguous().cuda()
+    cands = torch.tensor(tokens, dtype=torch.int32).expand(n, -1).contiguous().cuda()
+    # the borders of the third and fourth child, in 64 bits
+    left = np.exp(trees.log_softmax(t[0, 0].double().cpu().numpy(), 1.0))
+    borders = []
+    for x in tokens:
+        borders.append(left[x] / left.sum() if x >= 0 else 0.0)
+        if x >= 0:
+            left[x] = 0.0
+    rng = np.random.default_rng(1)
+    u = np.full((n, 5), 1 - 2.0 ** -24, np.float32)
+    for r in range(n):
+        which = 2 + r % 2
+        off = (1.0 + 2.0 ** -20 * rng.random()) ** (1 if r % 4 < 2 else -1)
+        u[r, which] = np.float32(min(borders[which] * off, 1 - 2.0 ** -24))
+        # a float32 step is 2^-23 at most: numbers that round onto the border itself are left out
+        if abs(float(u[r, which]) - borders[which]) <= 2.0 ** -32 * borders[which]:
+            u[r, which] = 0.5
+        u[r, 4] = rng.random()
+    u = torch.from_numpy(u).cuda()
+    check(sampler.verify(t, cands, u, parents=[-1] * 4), t, cands, u, [-1] * 4)
