@@ -470,3 +470,36 @@ def test_children_after_near_certain_ones(sampler, dtype, n, V, tokens):
         u[r, 4] = rng.random()
     u = torch.from_numpy(u).cuda()
     check(sampler.verify(t, cands, u, parents=[-1] * 4), t, cands, u, [-1] * 4)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,k,vocab,branch", [(16, 8, 152064, 1), (4, 15, 50257, 3), (1, 31, 152064, 1), (64, 31, 1025, 2),
+                                              (1, 0, 152064, 1), (2, 4, 4097, 4)])
+def test_without_a_drafter_on_both_sides_of_one_launch(sampler, n, k, vocab, branch, dtype):
+    """One launch takes up to a workgroup per compute unit, as the last two do; the others take two."""
+    t, _, cands, u = inputs(n, k, vocab, branch, dtype, seed=n + k, noise=0.1, temperature=0.4)
+    ks = [k - (r % 3 if k > 3 else 0) for r in range(n)]
+    dev = torch.tensor(ks, dtype=torch.int32, device="cuda")
+    for temperature in (0.4, 1.0):
+        check(sampler.verify(t, cands, u, parents=heap(k, branch), ks=dev, temperature=temperature), t, cands, u, heap(k, branch),
+              None, temperature, ks=ks)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [262144, 262145, 300007, 1048576, 1048577, 1500001, 1 << 24])
+def test_large_vocabularies(vocab, dtype):
+    """Rows of more parts than a wave keeps (262,144 tokens) and more chunks
+    than a workgroup has threads (1,048,576), up to the most; tokens far up the
+    vocabulary, and rejected ones there."""
+    n, k = (2, 3) if vocab < 1 << 24 else (1, 2)
+    s = as2d.Sampler(n, k, vocab)
+    t, d, cands, u = inputs(n, k, vocab, 1, dtype, seed=3) if vocab < 1 << 22 else (
+        torch.randn((n, k + 1, vocab), generator=torch.Generator().manual_seed(1)).to(dtype).cuda(),) * 2 + (
+        torch.tensor([[vocab - 1, 5]], dtype=torch.int32).cuda(), torch.tensor([[0.9, 0.9, 0.999]]).cuda())
+    parents = [-1] * (k - 1) + [0]
+    cands[0, 0] = vocab - 1
+    t[0, 0, vocab - 1] = 10.0
+    u[0, 0], u[0, k] = 1 - 2.0 ** -24, 1 - 2.0 ** -20
+    for draft in (None, d):
+        check(s.verify(t, cands, u, parents=parents, draft_logits=draft), t, cands, u, parents, draft)
+    s.close()

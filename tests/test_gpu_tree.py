@@ -484,6 +484,40 @@ def test_passes_over_long_caches():
     m.close()
 
 
+@pytest.mark.parametrize("shape", [TINY, TINY_BF16], ids=lambda s: s.name)
+@pytest.mark.parametrize("keys", [1, 40, 127, 300, 900])
+def test_passes_over_short_caches_in_long_slots(shape, keys):
+    """The usual serving layout: slots of more than 2,048 positions, whose span
+    states a second launch joins, with little in them.  Every branch is its own
+    chain's to rounding, alone and among other requests."""
+    from dataclasses import replace
+    shape = replace(shape, name="long", n_q_heads=14, n_kv_heads=2, n_layers=1)
+    _, m = make_pair(shape, max_requests=3, max_kv_len=4096, max_k=31, oracle=False)
+    m.set_keep_logits(True)
+    rng = np.random.default_rng(keys)
+    ks = [31, 6, 13]
+    parents = [[int(rng.integers(-1, i)) for i in range(k)] for k in ks]
+    cands = [rng.integers(0, shape.vocab, k).tolist() for k in ks]
+
+    def start(r):
+        m.prefill(r, np.zeros(0, np.uint16), np.arange(keys + 5 * r, dtype=np.int32) % shape.vocab)
+    for r in range(3):
+        start(r)
+    m.verify_tree_batch([0, 1, 2], cands, parents)
+    got = [m.logits(r) for r in range(3)]
+    for r in range(3):
+        start(r)
+        m.verify_tree(r, cands[r], parents[r])
+        assert close(got[r], m.logits(r), shape), r
+        sees = trees.visible(parents[r])
+        for leaf in [i for i in range(ks[r]) if i not in parents[r]][:6]:
+            rows = np.flatnonzero(sees[leaf + 1])
+            start(r)
+            m.verify(r, [cands[r][i - 1] for i in rows[1:]])
+            assert close(got[r][rows], m.logits(r), shape), (r, leaf)
+    m.close()
+
+
 def test_no_child_is_accepted(model):
     shape, m = model
     _, L = prefilled(m, shape)
