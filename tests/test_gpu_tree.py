@@ -157,6 +157,25 @@ def test_a_key_of_nan_is_never_passed_over(served, keys):
         assert torch.isnan(got[sees]).all(), row
 
 
+@pytest.mark.parametrize("keys", [2080, 2144, 2528, 4064])
+def test_a_key_of_nan_in_runs_of_keys(served, keys):
+    """The same with enough rows for runs of keys per workgroup (bf16 models), and values of NaN and infinity."""
+    shape, m = served
+    parents = heap(31, 3)
+    q, k, v, K, V = tensors(shape, 32, keys, 9)
+    m.prefill(0, np.zeros(0, np.uint16), np.zeros(keys, np.int32))
+    m.write_kv(0, 1, K, V)
+    clean = m.tree_attention(0, 1, q, k, v, parents)
+    for row in (0, 1, 9, 31):
+        sees = trees.visible(parents)[:, row]
+        for value, which in ((float("nan"), "k"), (float("nan"), "v"), (-float("inf"), "v")):
+            kk, vv = k.clone(), v.clone()
+            (kk if which == "k" else vv)[row, :, 5 if which == "v" else slice(None)] = value
+            got = m.tree_attention(0, 1, q, kk, vv, parents)
+            assert torch.equal(got[~sees], clean[~sees]), (row, which)
+            assert torch.isnan(got[sees]).all(), (row, which)
+
+
 LONG = [QWEN05B, QWEN7B]
 
 
