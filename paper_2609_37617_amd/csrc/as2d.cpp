@@ -442,23 +442,52 @@ bool wave_tiles(const as2d_ctx* c, int M, const ReqDesc* reqs, int n, int part_s
   return items > 2 * (c->grid_cus > 0 ? std::min(c->grid_cus, kAttnGrid) : kAttnGrid);
 }
 
-// Whether the attention of rows in trees takes runs of keys per workgroup
-// (attn_tree.hip) instead of 128 keys and 16 rows (attn_group_items): past as
-// many (span, KV head, row tile) items as the latter has workgroups, where one
-// launch does not join the states anyway.  A call of as2d_tree_attention,
-// groups against runs: 7B heads, 1 row over 8,000 keys (252 items) 17.6 us
+// How the attention of rows in trees runs (bf16 models): 0 with 128 keys and 16
+// rows per workgroup (attn_group_items), or with runs of keys per workgroup
+// (attn_tree.hip) of 1 or 2 row tiles a wave; `op`: a call of
+// as2d_tree_attention, else a pass, whose queries have low parts.
+//
+// Runs take over past as many (span, KV head, row tile) items as the groups
+// have workgroups, where one launch does not join the states anyway.  Groups
+// against runs, a call: 7B heads, 1 row over 8,000 keys (252 items) 17.6 us
 // against 18.6, over 16,000 (500) 25.0 against 23.6; 9 rows over 4,000 (512)
 // 18.0 against 18.3, over 8,000 (1,008) 26.0 against 21.3; 17 rows over 2,100
 // (544) 23.6 against 22.4; 3B heads, 17 rows over 2,100 (306) 18.1 against
 // 22.0, over 4,000 (576) 23.6 against 21.6; 0.5B heads, 32 rows over 2,100 (476)
-// 16.9 against 18.3, over 4,000 (896) 20.8 against 18.4.
-bool tree_by_runs(const as2d_ctx* c, const ReqDesc* reqs, int n, int part_spans) {
-  if (!c->bf16 || c->attn_rt || merge_last(part_spans)) return false;
-  const int hpg = c->cfg.n_q_heads / c->cfg.n_kv_heads;
-  long long items = 0;
-  for (int r = 0; r < n; ++r)
-    items += (long long)c->cfg.n_kv_heads * ((hpg * reqs[r].W + 15) / 16) * ((reqs[r].L0 + reqs[r].W - 1) / kAttnSpanKeys + 1);
-  return items > 2 * (c->grid_cus > 0 ? std::min(c->grid_cus, kAttnGrid) : kAttnGrid);
+// 16.9 against 18.3, over 4,000 (896) 20.8 against 18.4.  The two kernels of a
+// pass: 7B heads, 9 rows over 4,000 16.2 against 17.8, over 8,000 25.9 against
+// 21.0; 17 rows over 2,100 23.7 against 24.2; 3B heads, 17 rows over 2,100 15.9
+// against 23.1, over 4,000 23.8 against 23.6; 0.5B heads, 32 rows over 2,100 11.6
+// against 15.7, over 4,000 16.7 against 16.6; four and 16 requests of 9 rows over
+// 2,500 33.2 against 31.3 and 92.3 against 50.8.
+//
+// Two tiles a wave read a workgroup's keys from the LDS once for twice the
+// rows, but leave half as many workgroups to share the keys and twice the
+// states of a row to join: only where a KV head's rows fill more than one
+// tile a wave (64), and past four (span, KV head, 64 rows) items per compute
+// unit, or eight of a pass (whose scores take three products and not two).  One
+// tile against two, both kernels of a call: 7B heads over 8,000 keys, 18 rows
+// (504 items) 23.0 us against 28.1, 24 rows (756) 28.6 against 28.2, 32 (1,008)
+// 29.5 against 29.2; 10 rows over 20,000 (1,256) 33.9 against 33.7, over 30,000
+// (1,880) 44.0 against 38.6, 32 rows (3,760) 70.9 against 59.4; 0.5B heads, 32
+// rows over 16,000 (1,008) 23.7 against 25.5, over 30,000 (1,880) 35.6 against
+// 31.6.  Of a pass, 7B heads: 17 rows over 16,000 (1,008) 31.2 against 35.8, over
+// 30,000 (1,880) 44.9 against 46.6; 32 rows over 16,000 (2,016) 45.4 against 45.0,
+// over 30,000 (3,760) 68.9 against 64.5; four requests of 32 rows over 8,000
+// (4,032) 80.0 against 71.4; 16 requests of 9 rows, 63 a KV head, over 2,500 42.8
+// against 51.2.
+int tree_tiles(const as2d_ctx* c, const ReqDesc* reqs, int n, int part_spans, bool op) {
+  if (!c->bf16 || c->attn_rt || merge_last(part_spans)) return 0;
+  const int hpg = c->cfg.n_q_heads / c->cfg.n_kv_heads, cus = c->grid_cus > 0 ? std::min(c->grid_cus, kAttnGrid) : kAttnGrid;
+  long long items = 0, wide = 0;
+  bool fill = false;
+  for (int r = 0; r < n; ++r) {
+    const long long heads = (long long)c->cfg.n_kv_heads * ((reqs[r].L0 + reqs[r].W - 1) / kAttnSpanKeys + 1);
+    items += heads * ((hpg * reqs[r].W + 15) / 16);
+    wide += heads * ((hpg * reqs[r].W + 63) / 64);
+    fill |= hpg * reqs[r].W > 64;
+  }
+  return items <= 2 * cus ? 0 : fill && wide > (op ? 4 : 8) * cus ? 2 : 1;
 }
 
 // Kernel launches of one forward pass over the rows and requests in the
@@ -468,9 +497,9 @@ bool tree_by_runs(const as2d_ctx* c, const ReqDesc* reqs, int n, int part_spans)
 // (one request, its rows in order): its head runs over the last row tile
 // only, whose first row becomes row 0 of the logits and arg-max buffers.  max_blocks bounds the
 // attention key blocks of any request (it sizes the attention grid); tiles:
-// wave_tiles of the pass.
+// wave_tiles or tree_tiles of the pass.
 int launch_pass(as2d_ctx* c, const PassBufs& B, int M, int n_att, int n_fin, int fin_rows, bool with_head,
-                int max_blocks, bool prefill, bool tiles, PassRows tree = kPassVerify) {
+                int max_blocks, bool prefill, int tiles, PassRows tree = kPassVerify) {
   const as2d_config& g = c->cfg;
   hipStream_t s = c->stream;
   const bool bf = c->bf16;
@@ -760,11 +789,11 @@ int launch_persistent(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows) {
 // requests (fin_rows rows verified), captured on first use.  Kernel
 // arguments hold only pointers and sizes (the row and request descriptors
 // are read from device memory when the graph runs) and the attention grid
-// covers the slot capacity, so one graph (two with `tiles`, wave_tiles of the
-// pass, and as many for each of PassRows) serves every pass of that shape.
-int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persistent, bool tiles, PassRows tree,
+// covers the slot capacity, so one graph (one for each value of `tiles`,
+// wave_tiles or tree_tiles of the pass, and of PassRows) serves every pass of that shape.
+int graph_for(as2d_ctx* c, int M, int n_att, int n_fin, int fin_rows, bool persistent, int tiles, PassRows tree,
               hipGraphExec_t* out) {
-  const auto key = std::make_tuple((int)persistent, M, n_att, 4 * (int)tree + 2 * (int)tiles + c->keep_logits);
+  const auto key = std::make_tuple((int)persistent, M, n_att, 8 * (int)tree + 2 * tiles + c->keep_logits);
   auto it = c->graphs.find(key);
   if (it == c->graphs.end()) {
     if (c->graphs.size() >= 128) {
@@ -830,9 +859,9 @@ int run_forward(as2d_ctx* c, int M, int n_att, int n_fin, bool with_head, bool v
     HIP_TRY(c, hipMemcpyAsync(c->b.d_rows, c->h_rows, sizeof(RowDesc) * M, hipMemcpyHostToDevice, s));
     HIP_TRY(c, hipMemcpyAsync(c->b.d_reqs, c->h_reqs, sizeof(ReqDesc) * 2 * mr, hipMemcpyHostToDevice, s));
   }
-  const bool tiles = verify_call && !persistent &&
-                     (tree == kPassTrees ? tree_by_runs(c, c->h_reqs, n_att, c->b.part_spans)
-                                         : wave_tiles(c, M, c->h_reqs, n_att, c->b.part_spans));
+  const int tiles = !verify_call || persistent ? 0
+                    : tree == kPassTrees       ? tree_tiles(c, c->h_reqs, n_att, c->b.part_spans, false)
+                                               : wave_tiles(c, M, c->h_reqs, n_att, c->b.part_spans);
   if (graph) {
     hipGraphExec_t ex = nullptr;
     int rc = graph_for(c, M, n_att, n_fin, fin_rows, persistent, tiles, tree, &ex);
@@ -1812,7 +1841,7 @@ int as2d_tree_attention(as2d_ctx* c, int32_t req, int32_t layer, int32_t n_rows,
   t.merge_last = merge_last(spans);
   t.attn_cnt = c->b.attn_cnt;
   t.M = n_rows;
-  t.wave_tiles = tree_by_runs(c, &rq, 1, spans);
+  t.wave_tiles = tree_tiles(c, &rq, 1, spans, true);
   t.attn_rt = c->attn_rt;
   t.cus = c->grid_cus;
   HIP_TRY(c, launch_tree_attention(c->bf16, t, op, blocks, s));

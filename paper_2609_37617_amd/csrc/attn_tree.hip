@@ -343,19 +343,17 @@ template <int D, int T> static hipError_t tree_pass(const AttnArgs& a, int n_req
   return hipGetLastError();
 }
 
-// Two tiles a wave where a request's rows of a KV head need more than one.
-static bool two_tiles(const AttnArgs& a, int rows) { return a.n_q / a.n_kv * rows > 64; }
-
+// a.wave_tiles: row tiles a wave.
 hipError_t launch_tree_op(const AttnArgs& a, const TreeOp& op, int grid, hipStream_t s) {
   if (op.W < 1 || op.W > 32 || grid < 1) return hipErrorInvalidValue;
-  const bool two = two_tiles(a, op.W);
+  const bool two = a.wave_tiles == 2;
   if (a.head_dim == 128) return two ? tree_op<128, 2>(a, op, grid, s) : tree_op<128, 1>(a, op, grid, s);
   if (a.head_dim == 64) return two ? tree_op<64, 2>(a, op, grid, s) : tree_op<64, 1>(a, op, grid, s);
   return hipErrorInvalidValue;
 }
 hipError_t launch_tree_pass(const AttnArgs& a, int n_reqs, int grid, hipStream_t s) {
   if (n_reqs < 1 || grid < 1) return hipErrorInvalidValue;
-  const bool two = two_tiles(a, a.M - n_reqs + 1);   // a request's rows at most: one graph serves every pass of M rows
+  const bool two = a.wave_tiles == 2;
   if (a.head_dim == 128) return two ? tree_pass<128, 2>(a, n_reqs, grid, s) : tree_pass<128, 1>(a, n_reqs, grid, s);
   if (a.head_dim == 64) return two ? tree_pass<64, 2>(a, n_reqs, grid, s) : tree_pass<64, 1>(a, n_reqs, grid, s);
   return hipErrorInvalidValue;

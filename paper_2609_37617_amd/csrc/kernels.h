@@ -202,7 +202,7 @@ struct AttnArgs {
   int M;
   int tree;              // verification passes: rows see the committed keys and the request's rows in their mask
   int wave_tiles;        // verification passes of bf16 models: a row tile per wave (attn_spans_wide_kernel), or
-                         // of trees runs of keys per workgroup (attn_tree.hip)
+                         // of trees the row tiles a wave of runs of keys (attn_tree.hip)
   int attn_rt;           // row tiles per block of the verification kernel (0: chosen per launch)
   int cus;               // compute units the verification kernels may fill (the CU budget)
 };

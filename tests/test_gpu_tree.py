@@ -191,6 +191,47 @@ def test_attention_over_long_caches(shape, keys, rows, branch):
     m.close()
 
 
+@pytest.mark.parametrize("shape,keys,rows,branch", [(QWEN7B, 12345, 32, 2), (QWEN7B, 20001, 10, 3), (QWEN3B, 20000, 31, 2),
+                                                    (QWEN05B, 20000, 32, 5)], ids=str)
+def test_attention_of_two_row_tiles_a_wave(shape, keys, rows, branch):
+    """Caches long enough for two tiles, the second partly or wholly past the rows."""
+    m = heads_model(shape, keys + 64, max_requests=1)
+    attend_and_check(m, shape, keys, rows, heap(rows - 1, branch), keys + rows)
+    m.close()
+
+
+@pytest.mark.parametrize("cus", [2, 16, 64])
+def test_passes_of_two_row_tiles_a_wave(cus):
+    """With few compute units passes over 3,000 keys take two tiles: logits are
+    those of all units to rounding, for one request, three, and a graph of
+    either used in turn."""
+    from dataclasses import replace
+    shape = replace(TINY_BF16, name="long", n_q_heads=28, n_kv_heads=4, head_dim=128, n_layers=1)
+    _, m = make_pair(shape, max_requests=3, max_kv_len=4096, max_k=31, oracle=False)
+    m.set_keep_logits(True)
+    rng = np.random.default_rng(7)
+    ks = [31, 9, 2]   # the last two fill one tile each
+    parents = [[int(rng.integers(-1, i)) for i in range(k)] for k in ks]
+    cands = [rng.integers(0, shape.vocab, k).tolist() for k in ks]
+
+    def start():
+        for r in range(3):
+            m.prefill(r, np.zeros(0, np.uint16), np.arange(3000 + 300 * r, dtype=np.int32) % shape.vocab)
+
+    def passes():
+        out = []
+        for reqs in ([0], [0, 1, 2], [1, 2], [1], [0]):
+            start()
+            m.verify_tree_batch(reqs, [cands[r] for r in reqs], [parents[r] for r in reqs])
+            out += [m.logits(r) for r in reqs]
+        return out
+    want = passes()
+    m.set_cu_budget(cus)
+    for a, b in zip(want, passes()):
+        assert close(a, b, shape)
+    m.close()
+
+
 def test_attention_of_other_strides(served):
     """Heads before rows, rows further apart, an output inside a larger tensor."""
     shape, m = served
