@@ -47,7 +47,7 @@ enum {
   AS2D_OK = 0,
   AS2D_EINVAL = -1,    /* bad argument: k, token id, request id, rollback length, null pointer */
   AS2D_ECAPACITY = -2, /* the request's KV slot cannot hold the new rows */
-  AS2D_ESTATE = -3,    /* verify/decode on a request that has not been prefilled */
+  AS2D_ESTATE = -3,    /* a call on a request that has not been prefilled, or of a stream's capture (where it says so) */
   AS2D_EHIP = -4,      /* HIP runtime error */
   AS2D_ENUMERIC = -5,  /* non-finite logits: no token can be chosen */
   AS2D_ENOMEM = -6     /* device or pinned host allocation failed */
@@ -198,7 +198,9 @@ int as2d_verify_static(as2d_ctx* ctx, int32_t req, const int32_t* cands, int32_t
  * Passes over trees run as AS2D_EXEC_GRAPH where the mode is
  * AS2D_EXEC_PERSISTENT.  A sampling call allocates device memory at its first
  * use and when a call needs more (the drafter's logits it copies, and a
- * workspace of about 40 bytes per row and 4,096 tokens).
+ * workspace of 32 bytes per row and 1,024 tokens, 8 more for each child of a
+ * node but the first).  A call that fails has run nothing of the pass, or has
+ * been waited for; the request is as it was.
  */
 typedef struct {
   double temperature;        /* 1e-30 to 1e30: p = softmax(logits / temperature) */
@@ -219,15 +221,16 @@ int as2d_verify_tree_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const 
 
 /*
  * Operators on one layer of a request's cache, for programs that run layers of
- * their own beside the library (draft heads that read the target's cache,
- * caches that arrive from another process).  Tensors are memory of the
- * context's device (the current one at as2d_load_weights), [rows][heads][head_dim] with adjacent dimensions and any row and head
- * strides (in elements).  The call is ordered on hip_stream (NULL: the default
- * stream) of the context's device and returns before it has run; the
- * context's other calls wait for it, and these calls for each other, whatever
- * their streams.  They cannot be captured into a graph (AS2D_ESTATE; so do
- * calls that would have to wait for one whose stream is being captured by now).
- * Streams restricted by a CU mask are refused, as in as2d_set_stream (AS2D_EINVAL).
+ * their own beside the library (draft heads that read the target's cache, rows
+ * of a cache that another process has filled).  Tensors are memory of the
+ * context's device (the current one at as2d_load_weights),
+ * [rows][heads][head_dim] with adjacent dimensions and any row and head strides
+ * (in elements).  The call is ordered on hip_stream (NULL: the default stream)
+ * of the context's device and returns before it has run; the context's other
+ * calls wait for it, and these calls for each other, whatever their streams.
+ * They cannot be captured into a graph (AS2D_ESTATE; the same for a call that
+ * would have to wait for one whose stream is being captured by now).  Streams
+ * restricted by a CU mask are refused, as in as2d_set_stream (AS2D_EINVAL).
  *
  * as2d_tree_attention: attention of n_rows <= 32 rows of a tree (row 0 the
  * root; parents, host, n_rows - 1 entries or NULL, as above) over positions
@@ -244,7 +247,9 @@ int as2d_verify_tree_batch(as2d_ctx* ctx, int32_t n, const int32_t* reqs, const 
  *
  * as2d_write_kv: keys (rotated) and values of positions pos .. pos + n_tok - 1
  * <= kv_len - 1 of the layer, [n_tok][n_kv_heads][head_dim] in `dtype`
- * (AS2D_F32 or AS2D_BF16): the counterpart of as2d_read_kv.
+ * (AS2D_F32 or AS2D_BF16): the counterpart of as2d_read_kv.  A bf16 model's cache
+ * keeps them as pairs of bf16 (16 bits of a float32's 24).  The length is the
+ * request's own: a cache that is to be replaced whole is first prefilled to it.
  */
 typedef struct {
   void* data;
@@ -271,7 +276,8 @@ int as2d_write_kv(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t pos, int32_
  * and the walk goes on there; else R <- max(R - S q, 0), S <- sum R.  Without
  * draft_logits q is 1 at x: R(x) <- 0.  After the last child the token is the
  * first j with R_0 + .. + R_j > uniforms[k] S; where nothing is left of R, R = p
- * again.  Each committed token then follows p.
+ * again.  Each committed token then follows p; with draft_logits, if the
+ * children of a node are independent draws from q.
  *
  * A logit of -inf is a token of probability 0.  A request with a NaN or +inf
  * in a row (rows without children of draft_logits and rows past ks[r] are not
@@ -281,15 +287,14 @@ int as2d_write_kv(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t pos, int32_
  *
  * as2d_sampler_create allocates the workspace of calls of up to max_requests
  * <= 4096 requests, max_k <= 31 candidates and max_vocab <= 2^24 tokens on the
- * current device.  as2d_sampler_verify is ordered on hip_stream (none that a CU
- * mask restricts) and returns
- * before it has run; it may be captured into a graph.  Calls of one sampler
- * share the workspace: calls on several streams are ordered by the library
- * (AS2D_ESTATE where the last call's stream is being captured by now: what ran
- * there before cannot be waited for), captured calls by whoever replays the
- * graphs.  One host thread at a time.  Errors: AS2D_EINVAL, AS2D_ESTATE,
- * AS2D_EHIP, AS2D_ENOMEM; as2d_sampler_last_error(NULL) has the message of a
- * failed create.
+ * current device.  as2d_sampler_verify is ordered on hip_stream (AS2D_EINVAL if
+ * a CU mask restricts it) and returns before it has run; it may be captured into
+ * a graph.  Calls of one sampler share the workspace: calls on several streams
+ * are ordered by the library (AS2D_ESTATE where the last call's stream is being
+ * captured by now: what ran there before cannot be waited for), captured calls
+ * by whoever replays the graphs.  One host thread at a time.  Errors:
+ * AS2D_EINVAL, AS2D_ESTATE, AS2D_EHIP, AS2D_ENOMEM;
+ * as2d_sampler_last_error(NULL) has the message of a failed create.
  */
 typedef struct as2d_sampler as2d_sampler;
 

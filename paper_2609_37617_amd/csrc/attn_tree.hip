@@ -18,10 +18,11 @@
 // What bounds it: 64 keys of a head are 64 KiB, read by the LDS eight times
 // (2,048 cycles a step at 128 bytes a cycle) and multiplied by 16 T + 24 T
 // products a wave (two waves on each SIMD: 1,280 T cycles), so two tiles a wave
-// balance the two; one tile leaves the LDS as the limit.  Measured, 7B heads, 32
-// rows (224 per KV head): over 7,564 keys 23 us and 6 us for the join (one layer;
-// the cache's 31 MB at a copy's 5.1 TB/s: 6 us), over 32,704 keys 55.5 and 6.5
-// (134 MB: 26 us); workgroups of 128 keys and 16 rows took 68 and 225.  A step
+// balance the two; one tile leaves the LDS as the limit, but shares the keys among
+// twice the workgroups (as2d.cpp has the rule).  Measured, 7B heads, 32 rows (224
+// per KV head): over 7,564 keys, one tile, 24.5 us and 5 us for the join (one
+// layer; the cache's 31 MB at a copy's 5.1 TB/s: 6 us), over 32,704 keys, two
+// tiles, 55.5 and 6.5 (134 MB: 26 us); workgroups of 128 keys and 16 rows took 68 and 225.  A step
 // of 64 keys takes 2.7 us: the loads alone 2.5 (a step's burst, one in flight),
 // the products and powers alone 2.3, matrix cores a quarter busy.  All rows of a
 // KV head in one workgroup with two smaller steps in flight (256 rows): 55 us and

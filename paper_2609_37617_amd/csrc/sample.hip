@@ -9,29 +9,34 @@
 // walk goes on at the child; else R <- max(R - S q, 0), S <- sum of R.  Without
 // a drafter's row the child is certain, q(x) = 1 and 0 elsewhere: R(x) <- 0.
 // After the last child the token is the first j with R_0 + .. + R_j > u S.  The
-// token then has the target's distribution whatever the candidates are.
+// committed token then has the target's distribution: without a drafter's row
+// whatever the candidates are, with one if they are independent draws from it
+// (a tree of a row's most likely tokens is biased).
 //
 // Two rejections subtract a q, then b q; max(max(p - a q, 0) - b q, 0) =
 // max(p - (a + b) q, 0), so a node's state is the single number C (the sum of
 // the masses so far) and a mass is one pass over two rows:
 //   R = max(p - C q, 0),  C_1 = 1, C_{m+1} = C_m + S(C_m).
-// Masses after one rejection depend on no random number, so they are
-// computed for every node with a second child at once, and so on: as many
-// passes as the most children of a node, less one, and none for a chain.
+// A mass needs nothing from the walk, so those of one rejection are formed for
+// every node with a second child at once (that reject their first: its test is
+// made on the way), and so on: as many passes as the most children of a node,
+// less one, and none for a chain.  Without a drafter's row a mass is the row's
+// sum without the rejected tokens.
 //
 // What bounds it: few rows, latency (a chain of 8, 9 rows of 152,064 logits, 5.5
-// MB: 1.1 us at a copy's 5.1 TB/s; 13.8 us in one launch: start 2.5, the pass
-// 2, the last workgroup's ticket and the rows' parts 3, tests 1, the token's
-// chunk and column 4); many rows, the pass over them (16 requests, 13 rows of
-// each that matter, 126 MB: 25 us, 5.1 TB/s, and 16 for those of the 64 nodes
-// with a second child whose first is rejected: their two rows are read again,
-// and 14 to finish).
+// MB: 1.1 us at a copy's 5.1 TB/s; 15.1 us in one launch: its start, the pass,
+// the last workgroup's ticket and the rows' parts, the tests, the token's chunk
+// and column, each waiting for the one before); many rows, the pass over them
+// (16 requests, 13 rows of each that matter, 126 MB: 31 us, 4.1 TB/s, two thirds
+// of it 64-bit operations, 17 a logit; 18.9 for those of the 64 nodes with a
+// second child whose first is rejected: their two rows are read again; and 16
+// to finish).
 //
 // Rounding.  Powers are good to 2^-33.8 and everything summed over a row,
 // compared or logged has 64 bits, so that a random number falls on another side
-// of a border than in exact arithmetic only within 2^-33 of it: a draw from
-// 152,064 tokens then differs with a probability near 10^-6 (with float32 powers
-// it was 3 10^-4).
+// of a border than in exact arithmetic only within 2^-31 of it: a draw from
+// 152,064 tokens differs with a probability of 10^-7.  (float32 powers: 3 10^-4;
+// the pass over 126 MB 25 us, the whole call of a chain 13.9.)
 #include "common.h"
 
 namespace as2d {
@@ -385,9 +390,9 @@ __device__ __forceinline__ double chunk_left(const SampleArgs& a, long long trow
 // all rejected (C < 0 marks the others: the walk never asks for theirs).  Its C
 // is the earlier C and the earlier mass.  What that test saves depends on how
 // often a first child is accepted: 16 requests of 8 candidates in twos over
-// 152,064 float32 logits took 21.5 us without it and 16.3 with it; 4 requests of
-// 15 in threes over 50,257 bf16 logits 8.1 a stage without it and 8.5 with it
-// (the whole call 36.5 and 36.1).
+// 152,064 float32 logits took 25.5 us without it and 18.9 with it; 4 requests of
+// 15 in threes over 50,257 bf16 logits 9.2 a stage without it and 8.9 with it
+// (the whole call 40.5 and 40.3).
 template <bool BF>
 __global__ __launch_bounds__(kWide) void sample_stage_kernel(const SampleArgs a, const int s) {
   __shared__ RowStat s_stat[2];
@@ -785,9 +790,10 @@ template <bool BF> __global__ __launch_bounds__(kWide) void sample_fused_kernel(
 }
 
 // Up to this many workgroups (one per compute unit) a call without a drafter is
-// one launch: 16 requests of one row of 152,064 logits (160 workgroups) 12.5 us
-// against 15.3 in two, 1 request of 32 rows (320) 21.7 against 18.9: past one
-// workgroup a unit the larger kernel's fewer waves hold the pass back.
+// one launch: 16 requests of one row of 152,064 logits (160 workgroups) 13.2 us
+// against 15.4 in two, 1 request of 32 rows (320) 23.7 against 21.4, 16 of 9
+// (1,440) 45.7 against 30.7: past one workgroup a unit the larger kernel's fewer
+// waves hold the pass back.
 constexpr long long kFusedBlocks = 256;
 
 template <bool BF> hipError_t run(const SampleArgs& a, bool draft, hipStream_t s) {
