@@ -276,8 +276,9 @@ int as2d_write_kv(as2d_ctx* ctx, int32_t req, int32_t layer, int32_t pos, int32_
  * and the walk goes on there; else R <- max(R - S q, 0), S <- sum R.  Without
  * draft_logits q is 1 at x: R(x) <- 0.  After the last child the token is the
  * first j with R_0 + .. + R_j > uniforms[k] S; where nothing is left of R, R = p
- * again.  Each committed token then follows p; with draft_logits, if the
- * children of a node are independent draws from q.
+ * again.  Probabilities are 64-bit numbers: below 2^-1074 they are 0.  Each
+ * committed token then follows p; with draft_logits, if the children of a node
+ * are independent draws from q.
  *
  * A logit of -inf is a token of probability 0.  A request with a NaN or +inf
  * in a row (rows without children of draft_logits and rows past ks[r] are not

@@ -736,21 +736,20 @@ template <bool BF, bool FUSED> __device__ __forceinline__ void sample_finish(con
     chunk = max(chunk, 0);
     // the chunk's columns, one per thread: each summed as its chunk's sum took it
     const int col = chunk * kSampleChunk + tid;
-    double v = 0.0, top = 0.0;
+    double v = 0.0;
     float y = -INFINITY;
-    if (!(taken > 0.0)) {   // relative to the chunk's largest logit, as its sum was
-      top = load_part<FUSED>(part + chunk).top;
-      rest /= Power(q.c)(top - t.top);
-    }
     if (col < a.vocab) {
       y = logit<BF>(a.target, trow + col);
       if (taken > 0.0) {
         v = left_of(Power(q.c)(y, t.top), ps, Power(q.dc)(logit<BF>(a.draft, drow + col), d.top), qs);
-      } else if (top > -INFINITY && !is_gone(col)) {
-        v = Power(q.c)(y, top);
+      } else {
+        const double top = load_part<FUSED>(part + chunk).top;
+        if (top > -INFINITY && !is_gone(col)) v = Power(q.c)(y, top) * Power(q.c)(top - t.top);
       }
     }
-    const int who = find_in_run(v, [&](double) { return rest; }, s_find, nullptr);
+    int who = find_in_run(v, [&](double) { return rest; }, s_find, nullptr);
+    if (who < 0)   // columns that are 0 one by one (2^-1075), their sum is not: the first of them
+      who = find_in_run(y > -INFINITY && !is_gone(col) ? 1.0 : 0.0, [](double) { return 0.0; }, s_find, nullptr);
     if (tid == max(who, 0)) give(min(col, a.vocab - 1), y);
   }
 }

@@ -503,3 +503,28 @@ def test_large_vocabularies(vocab, dtype):
     for draft in (None, d):
         check(s.verify(t, cands, u, parents=parents, draft_logits=draft), t, cands, u, parents, draft)
     s.close()
+
+
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_the_number_zero_takes_the_first_token_with_a_probability(sampler, with_draft):
+    """In 64 bits: tokens below 2^-1074 of the whole have none, wherever in the
+    vocabulary and in their chunk they stand; candidates of theirs are never
+    accepted."""
+    n, V = 4, 5000
+    g = torch.Generator().manual_seed(33)
+    t = -900.0 - 50.0 * torch.rand((n, 2, V), generator=g)      # e^-900: 0
+    t[:, :, 3000:4000] = -600.0 - 50.0 * torch.rand((n, 2, 1000), generator=g)   # e^-650: a number
+    t[1, :, 900] = -640.0
+    t[2, :, 2047] = -500.0
+    t[3, :, :10] = -float("inf")
+    t[:, :, 4990] = 0.0
+    d = t if with_draft else None
+    cands = torch.full((n, 1), 17, dtype=torch.int32)
+    u = torch.zeros((n, 2))
+    got = sampler.verify(t.cuda(), cands.cuda(), u.cuda(), draft_logits=None if d is None else d.cuda())
+    # (with the target's own logits as the drafter's nothing is left of a rejection, and the target's own are drawn from)
+    assert got["accepted"].tolist() == [0] * n
+    assert got["token"].tolist() == [3000, 900, 2047, 3000]
+    for r in range(n):
+        p = np.exp(trees.log_softmax(t[r, 0].double().numpy(), 1.0))
+        assert int(np.argmax(np.cumsum(p) > 0)) == [3000, 900, 2047, 3000][r] and p[17] == 0
