@@ -321,15 +321,6 @@ void timing_collect(as2d_ctx* c) {
   c->ev_used.clear();
 }
 
-// Whether a stream is being captured: what ran on it before can then not be
-// waited for (an event recorded there would be a node of the caller's graph,
-// and a host wait would end the capture with an error).
-bool being_captured(hipStream_t s) {
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
-  (void)hipGetLastError();   // the stream may be gone
-  return false;
-}
 const char* const kOpCaptured = "the stream of the last operator on the cache is being captured: it cannot be waited for";
 
 // Waits for an operator that another call left running: every other call reads

@@ -27,6 +27,18 @@ struct OnDevice {
   }
 };
 
+// Whether a stream is being captured: what ran on it before can then not be
+// waited for (an event recorded there would be a node of the caller's graph,
+// and a host wait would end the capture with an error).  The null stream counts
+// as captured while a stream that it synchronises with is.
+inline bool being_captured(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  const hipError_t e = hipStreamIsCapturing(s, &st);
+  if (e == hipSuccess) return st != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();   // another error: the stream may be gone
+  return e == hipErrorStreamCaptureImplicit;
+}
+
 // Whether a stream is confined to part of the current device by a CU mask
 // (hipExtStreamCreateWithCUMask).  Such streams are refused: the first
 // concurrent run on masked streams ended in a host segmentation fault whose

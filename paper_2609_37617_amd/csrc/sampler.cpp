@@ -43,9 +43,7 @@ int hip_fail(as2d_sampler* s, const char* what, hipError_t e) {
 
 // The workspace is the last call's until it has run: stream st waits for it.
 hipError_t after_last(as2d_sampler* s, hipStream_t st) {
-  hipStreamCaptureStatus before = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s->last, &before) == hipSuccess && before != hipStreamCaptureStatusNone)
-    return hipErrorStreamCaptureUnsupported;   // an event recorded there would be a node of the caller's graph
+  if (being_captured(s->last)) return hipErrorStreamCaptureUnsupported;
   hipError_t e = hipEventRecord(s->ev, s->last);
   e = e == hipSuccess ? hipStreamWaitEvent(st, s->ev, 0) : hipDeviceSynchronize();   // the stream may be gone
   if (e == hipSuccess) (void)hipGetLastError();   // of the queries

@@ -100,6 +100,7 @@ hipError_t hipStreamCreateWithFlags(hipStream_t* s, unsigned) { return *s = rein
 hipError_t hipStreamDestroy(hipStream_t) { return hipSuccess; }
 hipError_t hipStreamGetDevice(hipStream_t s, hipDevice_t* d) { return *d = g_streams[num(s)].device, hipSuccess; }
 hipError_t hipStreamIsCapturing(hipStream_t s, hipStreamCaptureStatus* st) {
+  if (!s && g_streams[0].capturing) return error(hipErrorStreamCaptureImplicit);   // a stream it synchronises with is
   *st = g_streams[num(s)].capturing ? hipStreamCaptureStatusActive : hipStreamCaptureStatusNone;
   return hipSuccess;
 }

@@ -331,3 +331,17 @@ def test_the_device_is_the_one_at_creation(model, stub):
     model.write_kv(0, 0, k, k, stream=11)
     assert stub.lib.stub_device() == 1
     sampler.close()
+
+
+def test_the_default_stream_during_a_capture_it_takes_part_in(model, sampler, stub):
+    """The runtime gives an error, and no status, of the default stream while a stream that it synchronises with is captured."""
+    assert put(model, 0) == as2d.OK and sampler.verify(0) == as2d.OK
+    stub.stream(0, capturing=True)
+    stub.log()
+    state = model.state(0)
+    assert attend(model, 12) == sampler.verify(12) == as2d.ESTATE
+    refused(as2d.ESTATE, model.decode_one, 0)
+    assert order(stub.log()) == [] and model.state(0) == state and stub.pending_error() == 0
+    stub.stream(0)
+    assert attend(model, 12) == sampler.verify(12) == as2d.OK
+    assert order(stub.log()) == ["record 0", "wait 12", "launch tree_attention 12", "record 0", "wait 12", "launch sample 12"]
