@@ -365,6 +365,8 @@ hipError_t prepare_tree() {
   const auto allow = [&](const void* k) {
     if (e == hipSuccess) e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, tree_lds_bytes<128>());
   };
+  allow(reinterpret_cast<const void*>(&tree_op_kernel<64, 1>));   // 64 KiB, and the masks
+  allow(reinterpret_cast<const void*>(&tree_op_kernel<64, 2>));
   allow(reinterpret_cast<const void*>(&tree_op_kernel<128, 1>));
   allow(reinterpret_cast<const void*>(&tree_op_kernel<128, 2>));
   allow(reinterpret_cast<const void*>(&tree_pass_kernel<128, 1>));
